@@ -203,7 +203,7 @@ int atomo_entrywise_workspace_bytes(int64_t n, size_t* bytes /*host*/);
 
 /* Waits for `stream`, then reports and clears what the GPU latched since the last call:
  * ATOMO_OK, ATOMO_ECAPACITY, ATOMO_ENOCONV, ATOMO_EINVAL (an entry-wise or l_q message whose coordinates do not ascend
- * was decoded: the output is not its sum) or ATOMO_EHIP.  If sweeps is not NULL it receives the
+ * was decoded: the output is not its sum; or a token named no row of its table) or ATOMO_EHIP.  If sweeps is not NULL it receives the
  * largest number of Jacobi sweeps any matrix of the last atomo_encode_svd took. */
 int atomo_status(atomo_ctx* ctx, void* stream, int32_t* sweeps /*host, optional*/);
 int atomo_last_hip_error(const atomo_ctx* ctx);
@@ -322,6 +322,123 @@ int atomo_decode_svd_batch(atomo_ctx* ctx, const atomo_svd_msg* msgs, const int3
  */
 int atomo_apply_svd_batch(atomo_ctx* ctx, const atomo_svd_msg* msgs, const int32_t* first, int n_out,
                           float alpha, float* const* params, const int64_t* lds, void* stream);
+
+/* -------- the training step around the method ------------------------------------------------------
+ *
+ * What stands before and behind an encode / decode in the training of a language model: the embedding lookup with its
+ * gradient, which is a sum of row atoms e_token dy^T from the start, and the optimizer's step on the decoded gradients.
+ * The paper's own step is plain SGD (atomo_apply_svd_batch).
+ *
+ * Buffers that a call writes may not overlap others of that call.  Pointers need the alignment of their element type
+ * only.  All calls below may be captured into a graph, atomo_adamw_create apart.  Those that need the context's
+ * workspace (atomo_embedding_grad) do not grow it then: reserve it before (ATOMO_ENOMEM otherwise).  A block of
+ * workspace that a captured call uses stays allocated until atomo_destroy, also when a later call makes the context
+ * take a larger one; graphs of one context share it and must not run at the same time.  A captured call holds the
+ * numbers it was given; those that change from replay to replay come from device memory (step_dev, lr_dev). */
+
+enum { ATOMO_F32 = 0, ATOMO_BF16 = 1, ATOMO_F16 = 2 };
+
+/* A row-major matrix of ATOMO_F32 / BF16 / F16 elements: row stride ld >= cols elements (an input's may also be 0: every
+ * row the same; the stride of a single row is not looked at). */
+typedef struct atomo_rows {
+    int64_t rows;                    /* < 2^31 - 1; 0 rows only where stated                          */
+    int32_t cols, type;
+    int64_t ld;
+    void* data;                      /* device                                                        */
+} atomo_rows;
+
+/* A flat list of tokens, row numbers of the table.  Tokens that equal `padding` (any number, also one outside of the
+ * table) stand for no row. */
+typedef struct atomo_tokens {
+    int64_t n;                       /* 0 <= n < 2^31                                                 */
+    const void* data;                /* device: int32 or int64 [n]                                    */
+    int32_t bytes;                   /* 4 or 8 per token                                              */
+    int64_t padding;
+} atomo_tokens;
+
+/*
+ * Embedding lookup: out[t] = scale * table[tokens[t]], formed in fp32 and rounded once; zeros for padding.
+ *   out : tokens->n rows (at least; rows behind stay as they are) of table->cols columns, any of the types.
+ * A token outside of the table that is not padding gives zeros as well, and atomo_status reports ATOMO_EINVAL.
+ */
+int atomo_embedding(atomo_ctx* ctx, const atomo_rows* table /*host*/, const atomo_tokens* tokens /*host*/, float scale,
+                    const atomo_rows* out /*host*/, void* stream);
+
+/*
+ * Its gradient: grad[r] = (accumulate ? grad[r] : 0) + scale * sum over the t with tokens[t] = r of dy[t], summed in
+ * fp32 and rounded once to grad's type.  Without accumulate every row of grad is written, those that no token names as
+ * zeros; with it such rows are not touched.  The order of the sum depends on the sizes and the tokens alone, so the same
+ * call gives the same bits in every run.
+ *   dy : tokens->n rows (at least) of grad->cols columns.
+ * Tokens outside of the table are left out, and reported as by atomo_embedding.
+ */
+int atomo_embedding_grad(atomo_ctx* ctx, const atomo_tokens* tokens /*host*/, const atomo_rows* dy /*host*/, float scale,
+                         const atomo_rows* grad /*host*/, int accumulate, void* stream);
+
+/* Workspace of an atomo_embedding_grad of n_tokens into rows x cols. */
+int atomo_embedding_workspace_bytes(int64_t n_tokens, int64_t rows, int32_t cols, size_t* bytes /*host*/);
+
+/*
+ * AdamW over many tensors.  One step, t = 1, 2, ...:
+ *     g' = c g,  c = grad_scale * min(1, max_norm / *grad_norm)             (c = grad_scale without a norm to clip to)
+ *     m = beta1 m + (1 - beta1) g'        v = beta2 v + (1 - beta2) g' g'
+ *     param -= lr lr_mult / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps) + lr lr_mult weight_decay param
+ * in fp32, every product and sum of m and v rounded by itself; and, if it has one, copy = param rounded to copy_type.
+ * Where *grad_norm is not finite the step does nothing at all (the caller counts t on only where it was finite).
+ *
+ * States m and v are float32, or 8 bits per element with a scale for each block of 128 consecutive elements.  The scale
+ * is a byte S, the biased fp32 exponent of the block's largest finite |m| (v); E = max(S, 1) - 127.  m is a code of
+ * sign, 4 exponent bits (bias 7) and 3 mantissa bits times 2^(E - 7), its NaN being 0x7f; v, which is never negative, has
+ * 5 exponent bits (bias 15) and 3 mantissa bits, times 2^(E - 15), its NaN being 0xff.  Both are rounded at random such
+ * that their expectation is the value itself (to the nearest code, v could not follow: a step moves it by a
+ * thousandth, a code by an eighth): of an |x| that lies f steps of 2^-16 above a code, the next one is taken iff
+ * r + f >= 2^16, r uniform in 0 .. 2^16 - 1.  A v that is not zero keeps a code that is not zero.  Infinite and NaN
+ * values become NaN.  Element i of the tensor whose predecessors in the plan fill b blocks takes word i mod 4 of the Philox block with
+ * counter (32 b + i div 4, t) and key seed: r is its low half for m, its high half for v.
+ */
+typedef struct atomo_adamw_tensor {
+    int64_t n;                       /* elements, 0 < n < 2^40                                        */
+    float* param;                    /* [n]; NULL (in every tensor of a plan): atomo_adamw_grad_norm only */
+    const void* grad;                /* [n] of grad_type                                              */
+    void* m;                         /* [n] float32, or codes (uint8) if the scales are not NULL      */
+    void* v;
+    uint8_t* m_scale;                /* [ceil(n / 128)], or NULL, both                                */
+    uint8_t* v_scale;
+    void* copy;                      /* [n] of copy_type, or NULL                                     */
+    int32_t grad_type, copy_type;
+    float lr_mult, weight_decay;     /* finite, not negative                                          */
+} atomo_adamw_tensor;
+
+typedef struct atomo_adamw_options {
+    double lr, beta1, beta2, eps;    /* lr >= 0, 0 <= beta < 1, eps >= 0, finite                      */
+    int64_t step;                    /* t >= 1 (not looked at if step_dev is not NULL)                */
+    const int64_t* step_dev;         /* device [1], optional: t (below 1 is taken for 1)              */
+    const float* lr_dev;             /* device [1], optional: taken instead of lr                     */
+    const float* grad_norm;          /* device [1], optional: see above                               */
+    float max_norm;                  /* > 0: clip to it (needs grad_norm); 0: do not clip             */
+    float grad_scale;                /* finite                                                        */
+    uint64_t seed;                   /* of the rounding of 8-bit states                               */
+} atomo_adamw_options;
+
+typedef struct atomo_adamw atomo_adamw;   /* opaque: the tensors of a model, described once on the device */
+
+/* Describes the tensors (HOST array of n, read during the call) on the context's device; waits for the device.  Memory that a step
+ * writes may overlap nothing else in the plan: ATOMO_EINVAL, as for tensors of more than 6.8e10 elements together.  Contents stay the caller's: nothing of them is kept.
+ * One plan must not be used from two streams at once.  Destroy it before its context. */
+int atomo_adamw_create(atomo_ctx* ctx, const atomo_adamw_tensor* tensors /*host*/, int n, atomo_adamw** out);
+int atomo_adamw_destroy(atomo_ctx* ctx, atomo_adamw* plan);
+
+/* norm[0] = |grad_scale| * the Euclidean norm of all gradients of the plan, summed in double precision in a fixed order.
+ * norm : device [1]. */
+int atomo_adamw_grad_norm(atomo_ctx* ctx, const atomo_adamw* plan, float grad_scale, float* norm, void* stream);
+
+int atomo_adamw_step(atomo_ctx* ctx, const atomo_adamw* plan, const atomo_adamw_options* opt /*host*/, void* stream);
+
+/* What 8-bit states stand for: out[i] = code times scale, rounded to `type` (exact in ATOMO_F32, and in ATOMO_BF16 down to
+ * its smallest normal number).  n elements from the start of a block, 0 < n < 2^34. */
+enum { ATOMO_STATE_M = 0, ATOMO_STATE_V = 1 };
+int atomo_state8_unpack(atomo_ctx* ctx, int which, const uint8_t* codes, const uint8_t* scales, int64_t n, int type,
+                        void* out, void* stream);
 
 #ifdef __cplusplus
 }

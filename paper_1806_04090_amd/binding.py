@@ -22,6 +22,9 @@ LIB_PATH = os.environ.get("ATOMO_LIB") or os.path.join(_HERE, "libatomo.so")
 
 ATOMO_OK, ATOMO_EINVAL, ATOMO_ECAPACITY, ATOMO_ENOCONV, ATOMO_EHIP, ATOMO_ENOMEM, ATOMO_ETOOLARGE = 0, -1, -2, -3, -4, -5, -6
 ATOMO_KIND_SVD, ATOMO_KIND_ENTRYWISE, ATOMO_KIND_LQ = 0, 1, 2
+ATOMO_F32, ATOMO_BF16, ATOMO_F16 = 0, 1, 2
+ATOMO_STATE_M, ATOMO_STATE_V = 0, 1
+STATE8_BLOCK = 128           # elements of an 8-bit state that share a scale
 
 
 class AtomoError(RuntimeError):
@@ -47,6 +50,26 @@ class atomo_ew_msg(C.Structure):
 class atomo_lq_msg(C.Structure):
     _fields_ = [("n", C.c_int64), ("capacity", C.c_int64), ("count", C.c_void_p), ("idx", C.c_void_p),
                 ("norm", C.c_void_p)]
+
+
+class atomo_rows(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int32), ("type", C.c_int32), ("ld", C.c_int64), ("data", C.c_void_p)]
+
+
+class atomo_tokens(C.Structure):
+    _fields_ = [("n", C.c_int64), ("data", C.c_void_p), ("bytes", C.c_int32), ("padding", C.c_int64)]
+
+
+class atomo_adamw_tensor(C.Structure):
+    _fields_ = [("n", C.c_int64), ("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("grad_type", C.c_int32),
+                ("copy_type", C.c_int32), ("lr_mult", C.c_float), ("weight_decay", C.c_float)]
+
+
+class atomo_adamw_options(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64),
+                ("step_dev", C.c_void_p), ("lr_dev", C.c_void_p), ("grad_norm", C.c_void_p), ("max_norm", C.c_float),
+                ("grad_scale", C.c_float), ("seed", C.c_uint64)]
 
 
 class atomo_svd_options(C.Structure):
@@ -92,7 +115,16 @@ def lib() -> C.CDLL:
         L.atomo_measure_mfma_fp32.argtypes = [vp, C.POINTER(C.c_double), vp]
         L.atomo_profile_enable.argtypes = [vp, C.c_int]
         L.atomo_profile_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
-        for name in ("atomo_debug_direct_groups", "atomo_debug_entrywise_counts", "atomo_last_counters", "atomo_svd_sweeps", "atomo_profile_enable", "atomo_profile_read", "atomo_create", "atomo_destroy", "atomo_reserve", "atomo_svd_workspace_bytes",
+        L.atomo_embedding.argtypes = [vp, vp, vp, C.c_float, vp, vp]
+        L.atomo_embedding_grad.argtypes = [vp, vp, vp, C.c_float, vp, C.c_int, vp]
+        L.atomo_embedding_workspace_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int32, C.POINTER(C.c_size_t)]
+        L.atomo_adamw_create.argtypes = [vp, vp, C.c_int, C.POINTER(vp)]
+        L.atomo_adamw_destroy.argtypes = [vp, vp]
+        L.atomo_adamw_grad_norm.argtypes = [vp, vp, C.c_float, vp, vp]
+        L.atomo_adamw_step.argtypes = [vp, vp, vp, vp]
+        L.atomo_state8_unpack.argtypes = [vp, C.c_int, vp, vp, C.c_int64, C.c_int, vp, vp]
+        for name in ("atomo_embedding", "atomo_embedding_grad", "atomo_embedding_workspace_bytes", "atomo_adamw_create", "atomo_adamw_destroy",
+                     "atomo_adamw_grad_norm", "atomo_adamw_step", "atomo_state8_unpack", "atomo_debug_direct_groups", "atomo_debug_entrywise_counts", "atomo_last_counters", "atomo_svd_sweeps", "atomo_profile_enable", "atomo_profile_read", "atomo_create", "atomo_destroy", "atomo_reserve", "atomo_svd_workspace_bytes",
                      "atomo_entrywise_workspace_bytes", "atomo_status", "atomo_last_hip_error", "atomo_probabilities",
                      "atomo_encode_svd", "atomo_encode_entrywise", "atomo_encode_entrywise_noalloc", "atomo_encode_lq", "atomo_decode",
                      "atomo_decode_svd_batch", "atomo_apply_svd_batch", "atomo_measure_mfma_fp32"):
@@ -307,7 +339,7 @@ class Context:
         _check(lib().atomo_reserve(self._h, nbytes), "atomo_reserve")
 
     KERNEL_CLASSES = ("svd_prepare", "svd_gram", "svd_eig", "svd_update", "svd_refresh", "svd_finalize", "decode_svd",
-                      "ew_hist", "ew_solve", "ew_sample", "ew_decode", "svd_thin", "svd_direct")
+                      "ew_hist", "ew_solve", "ew_sample", "ew_decode", "svd_thin", "svd_direct", "embedding", "adamw")
 
     def measure_mfma_fp32(self) -> float:
         """TFLOP/s of a loop of fp32 matrix-core instructions on this GPU (blocks for about a millisecond)."""
@@ -522,3 +554,225 @@ def atomo_apply_svd_batch(ctx: Context, groups: Sequence[Sequence[SvdMessage]], 
     _check(lib().atomo_apply_svd_batch(ctx._h, c_msgs, c_first, len(params), float(alpha), c_params, c_lds,
                                        _stream_handle(stream)), "atomo_apply_svd_batch")
     return params
+
+
+# ------------------------------------------------------------------- the training step around the method
+
+_TYPES = {torch.float32: ATOMO_F32, torch.bfloat16: ATOMO_BF16, torch.float16: ATOMO_F16}
+_PACK_ROWS = struct.Struct("qiiqQ").pack
+_PACK_TOKENS = struct.Struct("qQi4xq").pack
+_PACK_ADAMW_TENSOR = struct.Struct("qQQQQQQQiiff").pack
+_PACK_ADAMW_OPTIONS = struct.Struct("ddddqQQQffQ").pack
+assert struct.calcsize("qiiqQ") == C.sizeof(atomo_rows) and struct.calcsize("qQi4xq") == C.sizeof(atomo_tokens)
+assert struct.calcsize("qQQQQQQQiiff") == C.sizeof(atomo_adamw_tensor)
+assert struct.calcsize("ddddqQQQffQ") == C.sizeof(atomo_adamw_options)
+
+
+def _stream_of(ctx: Context, stream: Optional[torch.cuda.Stream]) -> int:
+    """The stream given, or the current one of the context's device (which need not be the current device)."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(ctx.device.index)
+    if stream.device != ctx.device:
+        raise ValueError(f"the stream is one of {stream.device}, the context of {ctx.device}")
+    return int(stream.cuda_stream)
+
+
+def _on_device(ctx: Context, t: torch.Tensor, what: str, types) -> int:
+    """Checks the type and the device of a tensor; returns its address."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in types:
+        raise TypeError(f"{what} must be a tensor of {' or '.join(str(x).replace('torch.', '') for x in types)}")
+    if t.device != ctx.device:
+        raise ValueError(f"{what} is on {t.device}, the context on {ctx.device}")
+    return t.data_ptr()
+
+
+def _flat(ctx: Context, t: torch.Tensor, what: str, types, n: Optional[int] = None) -> int:
+    """The same for a contiguous tensor (of n elements)."""
+    at = _on_device(ctx, t, what, types)
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"{what} has {t.numel()} elements, not {n}")
+    return at
+
+
+def _pack_rows(ctx: Context, t: torch.Tensor, what: str) -> bytes:
+    at = _on_device(ctx, t, what, _TYPES)
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{what} must be a 2-D tensor with unit column stride")
+    return _PACK_ROWS(shape[0], shape[1], _TYPES[t.dtype], stride[0] if shape[0] > 1 else shape[1], at)
+
+
+_TOKEN_TYPES = (torch.int64, torch.int32)
+
+
+def _pack_tokens(ctx: Context, tokens: torch.Tensor, padding: int) -> bytes:
+    at = _flat(ctx, tokens, "tokens", _TOKEN_TYPES)
+    return _PACK_TOKENS(tokens.numel(), at, tokens.element_size(), padding)
+
+
+def _as_rows(t: torch.Tensor, tokens: torch.Tensor, what: str) -> torch.Tensor:
+    """A tensor of the tokens' shape and one dimension more as one row per token (a view)."""
+    if t.dim() == 2:
+        return t
+    if t.shape[:-1] != tokens.shape:
+        raise ValueError(f"{what} must have one row per token")
+    try:
+        return t.view(tokens.numel(), t.shape[-1])
+    except RuntimeError:
+        raise ValueError(f"{what} must have rows at one distance from each other") from None
+
+
+def atomo_embedding(ctx: Context, table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0,
+                    out: Optional[torch.Tensor] = None, padding: int = -1, stream=None) -> torch.Tensor:
+    """out[t] = scale * table[tokens[t]] (formed in float32, rounded once), zeros for padding.
+
+    tokens: contiguous int64 or int32 of any shape.  out: one row per token (of the tokens' shape and one dimension
+    more, or 2-D, whose rows behind the last token stay as they are), float32, bfloat16 or float16 whatever the table is;
+    by default a new tensor of the table's type.  A token that is neither padding nor a row of the table gives zeros, and
+    Context.status() says so."""
+    c_table, c_tokens = _pack_rows(ctx, table, "table"), _pack_tokens(ctx, tokens, padding)
+    if out is None:
+        out = torch.empty(*tokens.shape, table.shape[1], dtype=table.dtype, device=table.device)
+    c_out = _pack_rows(ctx, _as_rows(out, tokens, "out"), "out")
+    _check(lib().atomo_embedding(ctx._h, c_table, c_tokens, scale, c_out, _stream_of(ctx, stream)), "atomo_embedding")
+    return out
+
+
+def atomo_embedding_grad(ctx: Context, tokens: torch.Tensor, dy: torch.Tensor, grad: torch.Tensor, scale: float = 1.0,
+                         accumulate: bool = False, padding: int = -1, stream=None) -> torch.Tensor:
+    """grad[r] = (grad[r] if accumulate else 0) + scale * the sum of the dy[t] with tokens[t] = r, in float32, rounded once.
+
+    dy: one row per token, as atomo_embedding's `out`.  grad: rows x cols of the table.  Rows that no token names are
+    written as zeros, or not touched with accumulate.  The same call gives the same bits in every run."""
+    c_tokens, c_grad = _pack_tokens(ctx, tokens, padding), _pack_rows(ctx, grad, "grad")
+    c_dy = _pack_rows(ctx, _as_rows(dy, tokens, "dy"), "dy")
+    _check(lib().atomo_embedding_grad(ctx._h, c_tokens, c_dy, scale, c_grad, 1 if accumulate else 0, _stream_of(ctx, stream)),
+           "atomo_embedding_grad")
+    return grad
+
+
+def embedding_workspace_bytes(n_tokens: int, rows: int, cols: int) -> int:
+    """What Context.reserve needs for atomo_embedding_grad (which allocates nothing while it is captured into a graph)."""
+    size = C.c_size_t(0)
+    _check(lib().atomo_embedding_workspace_bytes(n_tokens, rows, cols, C.byref(size)), "atomo_embedding_workspace_bytes")
+    return int(size.value)
+
+
+@dataclass
+class AdamwState:
+    """The averages m and v of one tensor: float32, or codes of 8 bits (uint8) with a scale for each 128 of them."""
+    m: torch.Tensor
+    v: torch.Tensor
+    m_scale: Optional[torch.Tensor] = None    # uint8 [ceil(n / 128)]
+    v_scale: Optional[torch.Tensor] = None
+
+
+def alloc_adamw_state(n: int, bits: int, device) -> AdamwState:
+    """The state of a tensor of n elements before the first step: zeros, in 32 or 8 bits."""
+    if bits == 32:
+        return AdamwState(*(torch.zeros(n, dtype=torch.float32, device=device) for _ in range(2)))
+    if bits != 8:
+        raise ValueError("states have 32 or 8 bits")
+    sizes = (n, n, -(-n // STATE8_BLOCK), -(-n // STATE8_BLOCK))
+    return AdamwState(*(torch.zeros(k, dtype=torch.uint8, device=device) for k in sizes))
+
+
+class AdamwPlan:
+    """Parameters, gradients and states of a model, described once for all steps; the tensors stay the caller's and are kept
+    alive by the plan.  A tensor that is given other memory needs a new plan.
+
+    params: contiguous float32 tensors, or None for a plan of gradients alone (atomo_adamw_grad_norm); grads: float32, bfloat16 or
+    float16 of the same sizes; copies: None, or for each tensor None or a bfloat16, float16 or float32 tensor that gets the rounded
+    parameters at every step; weight_decay, lr_mult: a number, or one per tensor."""
+
+    def __init__(self, ctx: Context, params: Optional[Sequence[torch.Tensor]], grads: Sequence[torch.Tensor],
+                 states: Optional[Sequence[AdamwState]] = None, copies: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                 weight_decay=0.0, lr_mult=1.0):
+        self._h, self._ctx = C.c_void_p(), ctx
+        n = len(grads)
+        decay, mult = (list(x) if isinstance(x, (list, tuple)) else [x] * n for x in (weight_decay, lr_mult))
+        copies = [None] * n if copies is None else list(copies)
+        if any(len(x) != n for x in (params or grads, states or grads, copies, decay, mult)):
+            raise ValueError("every list needs one entry per gradient")
+        if (params is None) != (states is None):
+            raise ValueError("parameters need states, and states parameters")
+        f32, u8 = (torch.float32,), (torch.uint8,)
+        blob = []
+        for j, g in enumerate(grads):
+            size, at, copy_type = g.numel(), [0] * 6, ATOMO_F32
+            if params is not None:
+                s = states[j]
+                at[0] = _flat(ctx, params[j], f"params[{j}]", f32, size)
+                if s.m_scale is None and s.v_scale is None:
+                    at[1], at[2] = (_flat(ctx, x, f"states[{j}]", f32, size) for x in (s.m, s.v))
+                else:
+                    blocks = -(-size // STATE8_BLOCK)
+                    at[1:5] = [_flat(ctx, x, f"states[{j}]", u8, k) for x, k in
+                               ((s.m, size), (s.v, size), (s.m_scale, blocks), (s.v_scale, blocks))]
+                if copies[j] is not None:
+                    at[5] = _flat(ctx, copies[j], f"copies[{j}]", _TYPES, size)
+                    copy_type = _TYPES[copies[j].dtype]
+            grad = _flat(ctx, g, f"grads[{j}]", _TYPES)
+            blob.append(_PACK_ADAMW_TENSOR(size, at[0], grad, *at[1:], _TYPES[g.dtype], copy_type, mult[j], decay[j]))
+        self._tensors = (params, list(grads), states, copies)
+        _check(lib().atomo_adamw_create(ctx._h, b"".join(blob), n, C.byref(self._h)), "atomo_adamw_create")
+
+    def close(self):
+        if self._h and self._ctx._h:
+            lib().atomo_adamw_destroy(self._ctx._h, self._h)
+        self._h, self._tensors = C.c_void_p(), None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+_ONE_F32, _ONE_I64 = (torch.float32,), (torch.int64,)
+
+
+def atomo_adamw_grad_norm(ctx: Context, plan: AdamwPlan, grad_scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                          stream=None) -> torch.Tensor:
+    """|grad_scale| times the Euclidean norm of all gradients of the plan, a float32 tensor [1] on the device."""
+    if out is None:
+        out = torch.empty(1, dtype=torch.float32, device=ctx.device)
+    at = _flat(ctx, out, "out", _ONE_F32, 1)
+    _check(lib().atomo_adamw_grad_norm(ctx._h, plan._h, grad_scale, at, _stream_of(ctx, stream)), "atomo_adamw_grad_norm")
+    return out
+
+
+def atomo_adamw_step(ctx: Context, plan: AdamwPlan, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, *, step,
+                     grad_scale: float = 1.0, grad_norm: Optional[torch.Tensor] = None, max_norm: float = 0.0, seed: int = 0,
+                     stream=None) -> None:
+    """One AdamW step of all tensors of the plan, in place (atomo.h has the formulas).
+
+    step: t = 1, 2, ..., a number or an int64 tensor [1] on the device; lr: a number or a float32 tensor [1] on the
+    device (a captured step reads such tensors at every replay).  grad_norm: what atomo_adamw_grad_norm gave for the
+    same grad_scale; the step does nothing where it is not finite, and clips to max_norm if that is above 0.  seed: of the rounding
+    of 8-bit states."""
+    step_at = lr_at = 0
+    if isinstance(step, torch.Tensor):
+        step, step_at = 0, _flat(ctx, step, "step", _ONE_I64, 1)
+    if isinstance(lr, torch.Tensor):
+        lr, lr_at = 0.0, _flat(ctx, lr, "lr", _ONE_F32, 1)
+    norm_at = 0 if grad_norm is None else _flat(ctx, grad_norm, "grad_norm", _ONE_F32, 1)
+    options = _PACK_ADAMW_OPTIONS(lr, beta1, beta2, eps, step, step_at, lr_at, norm_at, max_norm, grad_scale, int(seed) & (2 ** 64 - 1))
+    _check(lib().atomo_adamw_step(ctx._h, plan._h, options, _stream_of(ctx, stream)), "atomo_adamw_step")
+
+
+def atomo_state8_unpack(ctx: Context, which: str, codes: torch.Tensor, scales: torch.Tensor,
+                        out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """What the codes of an 8-bit state stand for; which: "m" or "v".  out: float32 (the default) or 16 bits."""
+    if which not in ("m", "v"):
+        raise ValueError('which is "m" or "v"')
+    n = codes.numel()
+    if out is None:
+        out = torch.empty(n, dtype=torch.float32, device=codes.device)
+    u8 = (torch.uint8,)
+    _check(lib().atomo_state8_unpack(ctx._h, ATOMO_STATE_M if which == "m" else ATOMO_STATE_V, _flat(ctx, codes, "codes", u8),
+                                     _flat(ctx, scales, "scales", u8, -(-n // STATE8_BLOCK)), n, _TYPES[out.dtype] if isinstance(out, torch.Tensor) and out.dtype in _TYPES else -1,
+                                     _flat(ctx, out, "out", _TYPES, n), _stream_of(ctx, stream)), "atomo_state8_unpack")
+    return out

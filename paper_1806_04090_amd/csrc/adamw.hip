@@ -1,0 +1,520 @@
+// AdamW over many tensors, the norm of their gradients, and what 8-bit states stand for.
+//
+// Every element is read and written once and has about fourteen operations (twice that, and a third of a Philox block, with 8-bit
+// states): the bound is HBM, 28 bytes per element with 32-bit states and gradients, 16 with states in 8 bits.
+// The tensors of a plan are described once on the device; a step is one launch over chunks of CHUNK elements of all of
+// them (two, if both kinds of states occur).
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <memory>
+#include <vector>
+
+#include "element_types.h"
+
+namespace atomo {
+
+namespace {
+
+constexpr int CHUNK = 4096;            // elements of a workgroup of 256 threads, four times four per thread
+constexpr int BLOCK8 = 128;            // elements of an 8-bit state with one scale: four of each of 32 lanes
+constexpr int NORM_PARTS = 1024;       // partial sums of a norm
+
+struct Tensor {
+    float* param;
+    void* copy;
+    const void* grad;
+    void* m;
+    void* v;
+    uint8_t* m_scale;
+    uint8_t* v_scale;
+    long long n;
+    long long first_block;             // 8-bit blocks of the tensors in front
+    int grad_type, copy_type;
+    float lr_mult, weight_decay;
+};
+
+struct Chunk { int tensor, chunk; };   // elements [chunk * CHUNK, + CHUNK) of it
+
+// What a step needs besides the tensors.  Of beta^t a kernel forms what it needs itself if t lies on the device.
+struct StepArgs {
+    double lr, rate, beta1, beta2;     // rate = lr / (1 - beta1^t)
+    const long long* step_dev;
+    const float* lr_dev;
+    const float* grad_norm;
+    long long step;
+    uint64_t seed;
+    float b1, c1, b2, c2;              // beta and 1 - beta, rounded once each from double
+    float eps, root;                   // root = 1 / sqrt(1 - beta2^t)
+    float max_norm, grad_scale;
+};
+
+__device__ double power(double x, long long t)
+{
+    double r = 1.0;
+    for (; t > 0; t >>= 1, x *= x)
+        if (t & 1) r *= x;
+    return r;
+}
+
+// What is the same for all elements of a workgroup's tensor.
+struct Rates {
+    float gs, rate, decay, root;
+    long long step;
+};
+
+// false: the step is skipped
+__device__ inline bool rates_of(const StepArgs& a, const Tensor& t, Rates& r)
+{
+    float coefficient = 1.0f;
+    if (a.grad_norm) {
+        const float norm = *a.grad_norm;
+        if (!(norm <= 3.4028235e38f)) return false;              // (infinite or NaN)
+        if (a.max_norm > 0.0f && norm > a.max_norm) coefficient = a.max_norm / norm;
+    }
+    r.gs = a.grad_scale * coefficient;
+    double lr = a.lr, rate = a.rate;
+    r.root = a.root;
+    r.step = a.step;
+    if (a.lr_dev) lr = (double)*a.lr_dev;
+    if (a.step_dev) {
+        const long long given = *a.step_dev;
+        r.step = given < 1 ? 1 : given;
+        rate = lr / (1.0 - power(a.beta1, r.step));
+        r.root = (float)(1.0 / sqrt(1.0 - power(a.beta2, r.step)));
+    } else if (a.lr_dev) {
+        rate = lr / (1.0 - power(a.beta1, r.step));
+    }
+    r.rate = (float)(rate * (double)t.lr_mult);
+    r.decay = (float)(lr * (double)t.lr_mult * (double)t.weight_decay);
+    return true;
+}
+
+// One element.  The products and sums of m and v are rounded each by itself, without fused multiply-adds: the 8-bit codes
+// depend on the last bit, and this way they are the same as those of any program that forms the two sums in fp32.
+__device__ inline void adamw_element(const StepArgs& a, const Rates& r, float g, float& p, float& m, float& v)
+{
+#pragma clang fp contract(off)
+    g = g * r.gs;
+    m = a.b1 * m + a.c1 * g;
+    v = a.b2 * v + a.c2 * (g * g);
+    const float step = r.rate * (m / (sqrtf(v) * r.root + a.eps));
+    p = p - (step + r.decay * p);
+}
+
+__device__ inline f32x4 load_any4(int type, const void* base, long long i)
+{
+    return type == ATOMO_F32 ? load4<ATOMO_F32>(base, i) : type == ATOMO_BF16 ? load4<ATOMO_BF16>(base, i) : load4<ATOMO_F16>(base, i);
+}
+
+__device__ inline float load_any1(int type, const void* base, long long i)
+{
+    return type == ATOMO_F32 ? load1<ATOMO_F32>(base, i) : type == ATOMO_BF16 ? load1<ATOMO_BF16>(base, i) : load1<ATOMO_F16>(base, i);
+}
+
+__device__ inline void store_any4(int type, void* base, long long i, f32x4 x)
+{
+    if (type == ATOMO_F32) store4<ATOMO_F32>(base, i, x);
+    else if (type == ATOMO_BF16) store4<ATOMO_BF16>(base, i, x);
+    else store4<ATOMO_F16>(base, i, x);
+}
+
+__device__ inline void store_any1(int type, void* base, long long i, float x)
+{
+    if (type == ATOMO_F32) store1<ATOMO_F32>(base, i, x);
+    else if (type == ATOMO_BF16) store1<ATOMO_BF16>(base, i, x);
+    else store1<ATOMO_F16>(base, i, x);
+}
+
+__global__ __launch_bounds__(256) void adamw_states32(const Tensor* tensors, const Chunk* chunks, StepArgs a)
+{
+    const Chunk c = chunks[blockIdx.x];
+    const Tensor t = tensors[c.tensor];
+    Rates r;
+    if (!rates_of(a, t, r)) return;
+    const long long first = (long long)c.chunk * CHUNK;
+    float* const m = (float*)t.m;
+    float* const v = (float*)t.v;
+#pragma unroll
+    for (int k = 0; k < CHUNK / 1024; ++k) {
+        const long long i = first + k * 1024 + threadIdx.x * 4;
+        if (i + 4 <= t.n) {
+            const f32x4 g = load_any4(t.grad_type, t.grad, i);
+            f32x4 p4 = load4<ATOMO_F32>(t.param, i), m4 = load4<ATOMO_F32>(m, i), v4 = load4<ATOMO_F32>(v, i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float pe = p4[e], me = m4[e], ve = v4[e];
+                adamw_element(a, r, g[e], pe, me, ve);
+                p4[e] = pe; m4[e] = me; v4[e] = ve;
+            }
+            store4<ATOMO_F32>(t.param, i, p4);
+            store4<ATOMO_F32>(m, i, m4);
+            store4<ATOMO_F32>(v, i, v4);
+            if (t.copy) store_any4(t.copy_type, t.copy, i, p4);
+        } else {
+            for (long long j = i; j < t.n; ++j) {
+                float pe = t.param[j], me = m[j], ve = v[j];
+                adamw_element(a, r, load_any1(t.grad_type, t.grad, j), pe, me, ve);
+                t.param[j] = pe;
+                m[j] = me;
+                v[j] = ve;
+                if (t.copy) store_any1(t.copy_type, t.copy, j, pe);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// 8-bit states
+// ---------------------------------------------------------------------------------------------
+
+// A code of three mantissa bits lies in the top of an fp32 number: shifted there, its exponent bias is fp32's, so that
+// one exact scaling by a power of two gives its value (the smallest codes are fp32 denormals in between, which the instruction keeps).
+constexpr int M_BIAS = 7, V_BIAS = 15;
+constexpr int TO_FP32 = 127;
+
+__device__ inline int block_exponent(int scale) { return (scale > 1 ? scale : 1) - 127; }
+
+__device__ inline float m_value(uint32_t code, int e)
+{
+    const float x = ldexpf(__uint_as_float((code & 0x7f) << 20), TO_FP32 - M_BIAS + e - M_BIAS);
+    const float y = (code & 0x7f) == 0x7f ? __uint_as_float(0x7fc00000u) : x;
+    return code & 0x80 ? -y : y;
+}
+
+__device__ inline float v_value(uint32_t code, int e)
+{
+    const float x = ldexpf(__uint_as_float(code << 20), TO_FP32 - V_BIAS + e - V_BIAS);
+    return code == 0xff ? __uint_as_float(0x7fc00000u) : x;
+}
+
+// |x| scaled to where its code's exponent is fp32's; then adding r below the three mantissa bits carries into them with the
+// probability of what is cut off.  (Below the smallest normal code the scaled number is a denormal, rounded to 2^-20 of a step.)
+__device__ inline uint32_t code_of(float x, int exponent, uint32_t r)
+{
+    return (__float_as_uint(ldexpf(fabsf(x), exponent)) + (r << 4)) >> 20;
+}
+
+__device__ inline bool finite(float x) { return (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u; }
+
+__device__ inline uint32_t m_code(float x, int e, uint32_t r)
+{
+    const uint32_t c = finite(x) ? code_of(x, M_BIAS - e - (TO_FP32 - M_BIAS), r) : 0x7fu;
+    return c | (x < 0.0f ? 0x80u : 0u);
+}
+
+__device__ inline uint32_t v_code(float x, int e, uint32_t r)
+{
+    if (!finite(x)) return 0xffu;
+    const uint32_t c = code_of(x, V_BIAS - e - (TO_FP32 - V_BIAS), r);
+    return c == 0 && x > 0.0f ? 1u : c;                          // (a v of zero under an m that is not would be a step without bound)
+}
+
+__global__ __launch_bounds__(256) void adamw_states8(const Tensor* tensors, const Chunk* chunks, StepArgs a)
+{
+    const Chunk c = chunks[blockIdx.x];
+    const Tensor t = tensors[c.tensor];
+    Rates r;
+    if (!rates_of(a, t, r)) return;
+    const long long first = (long long)c.chunk * CHUNK;
+    uint8_t* const mc = (uint8_t*)t.m;
+    uint8_t* const vc = (uint8_t*)t.v;
+    for (int k = 0; k < CHUNK / 1024; ++k) {
+        const long long i = first + k * 1024 + threadIdx.x * 4;
+        if (first + k * 1024 + (threadIdx.x & ~63) * 4 >= t.n) break;          // (no lane of the wave has an element)
+        const long long block = i / BLOCK8;
+        const int left = (int)(t.n - i < 4 ? (t.n - i > 0 ? t.n - i : 0) : 4);
+        const bool any = left > 0;
+        float p[4] = {0, 0, 0, 0}, m[4], v[4], g[4] = {0, 0, 0, 0};
+        uint32_t mq = 0, vq = 0;
+        const int em = block_exponent(any ? t.m_scale[block] : 0), ev = block_exponent(any ? t.v_scale[block] : 0);
+        if (left == 4) {
+            const f32x4 p4 = load4<ATOMO_F32>(t.param, i), g4 = load_any4(t.grad_type, t.grad, i);
+            __builtin_memcpy(&mq, mc + i, 4);
+            __builtin_memcpy(&vq, vc + i, 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { p[e] = p4[e]; g[e] = g4[e]; }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < left) {
+                    p[e] = t.param[i + e];
+                    g[e] = load_any1(t.grad_type, t.grad, i + e);
+                    mq |= (uint32_t)mc[i + e] << (8 * e);
+                    vq |= (uint32_t)vc[i + e] << (8 * e);
+                }
+        }
+        uint32_t sm = 0, sv = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            m[e] = m_value(mq >> (8 * e) & 0xff, em);
+            v[e] = v_value(vq >> (8 * e) & 0xff, ev);
+            adamw_element(a, r, g[e], p[e], m[e], v[e]);
+            if (finite(m[e])) sm = max(sm, __float_as_uint(m[e]) >> 23 & 0xff);
+            if (finite(v[e])) sv = max(sv, __float_as_uint(v[e]) >> 23);
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            sm = max(sm, (uint32_t)__shfl_xor((int)sm, d));
+            sv = max(sv, (uint32_t)__shfl_xor((int)sv, d));
+        }
+        const int fm = block_exponent((int)sm), fv = block_exponent((int)sv);
+        const u32x4 w = philox4x32_10((uint64_t)(t.first_block * (BLOCK8 / 4) + i / 4), (uint64_t)r.step, a.seed);
+        const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+        mq = vq = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            mq |= m_code(m[e], fm, words[e] & 0xffff) << (8 * e);
+            vq |= v_code(v[e], fv, words[e] >> 16) << (8 * e);
+        }
+        if (left == 4) {
+            const f32x4 p4 = {p[0], p[1], p[2], p[3]};
+            store4<ATOMO_F32>(t.param, i, p4);
+            if (t.copy) store_any4(t.copy_type, t.copy, i, p4);
+            __builtin_memcpy(mc + i, &mq, 4);
+            __builtin_memcpy(vc + i, &vq, 4);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < left) {
+                    t.param[i + e] = p[e];
+                    if (t.copy) store_any1(t.copy_type, t.copy, i + e, p[e]);
+                    mc[i + e] = (uint8_t)(mq >> (8 * e));
+                    vc[i + e] = (uint8_t)(vq >> (8 * e));
+                }
+        }
+        if (any && (threadIdx.x & 31) == 0) {
+            t.m_scale[block] = (uint8_t)sm;
+            t.v_scale[block] = (uint8_t)sv;
+        }
+    }
+}
+
+template <int TYPE, bool V>
+__global__ __launch_bounds__(256) void state8_values(const uint8_t* codes, const uint8_t* scales, long long n, void* out)
+{
+    const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    const int e = block_exponent(scales[i / BLOCK8]);
+    if (i + 4 <= n) {
+        uint32_t q;
+        __builtin_memcpy(&q, codes + i, 4);
+        f32x4 x;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = V ? v_value(q >> (8 * k) & 0xff, e) : m_value(q >> (8 * k) & 0xff, e);
+        store4<TYPE>(out, i, x);
+    } else {
+        for (long long j = i; j < n; ++j) store1<TYPE>(out, j, V ? v_value(codes[j], e) : m_value(codes[j], e));
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// The norm of all gradients
+// ---------------------------------------------------------------------------------------------
+
+__device__ double workgroup_sum(double x)
+{
+    __shared__ double part[4];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return part[0] + part[1] + part[2] + part[3];
+}
+
+// Squares and sums in double precision: neither the square of a tiny gradient nor that of a huge one is lost.
+__global__ __launch_bounds__(256) void norm_parts(const Tensor* tensors, const Chunk* chunks, int n_chunks, double* parts)
+{
+    double sum = 0.0;
+    for (int b = blockIdx.x; b < n_chunks; b += gridDim.x) {
+        const Chunk c = chunks[b];
+        const Tensor& t = tensors[c.tensor];
+        const long long n = t.n;
+        const void* const grad = t.grad;
+        const int type = t.grad_type;
+        const long long first = (long long)c.chunk * CHUNK;
+#pragma unroll
+        for (int k = 0; k < CHUNK / 1024; ++k) {
+            const long long i = first + k * 1024 + threadIdx.x * 4;
+            if (i + 4 <= n) {
+                const f32x4 g = load_any4(type, grad, i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum = fma((double)g[e], (double)g[e], sum);
+            } else {
+                for (long long j = i; j < n; ++j) {
+                    const double g = (double)load_any1(type, grad, j);
+                    sum = fma(g, g, sum);
+                }
+            }
+        }
+    }
+    sum = workgroup_sum(sum);
+    if (threadIdx.x == 0) parts[blockIdx.x] = sum;
+}
+
+__global__ __launch_bounds__(256) void norm_total(const double* parts, int n, float scale, float* norm)
+{
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < n; i += 256) sum += parts[i];
+    sum = workgroup_sum(sum);
+    if (threadIdx.x == 0) norm[0] = (float)((double)scale * sqrt(sum));
+}
+
+}  // namespace
+
+}  // namespace atomo
+
+struct atomo_adamw {
+    int device = 0;
+    void* dev = nullptr;               // tables and partial sums, one block
+    atomo::Tensor* tensors = nullptr;
+    atomo::Chunk* chunks = nullptr;    // those of tensors with 32-bit states first
+    double* parts = nullptr;
+    int n32 = 0, n8 = 0;               // chunks
+    bool updates = false;              // has parameters
+};
+
+namespace atomo {
+
+// Whether something that a step writes overlaps anything else of the plan.
+bool adamw_overlap(const atomo_adamw_tensor* tensors, int n)
+{
+    struct Range { uintptr_t first, end; bool written; };
+    std::vector<Range> ranges;
+    const auto add = [&](const void* p, int64_t bytes, bool written) {
+        if (p) ranges.push_back(Range{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, written});
+    };
+    for (int j = 0; j < n; ++j) {
+        const atomo_adamw_tensor& t = tensors[j];
+        add(t.grad, t.n * type_bytes(t.grad_type), false);
+        if (!t.param) continue;
+        const int64_t state_bytes = t.n * (t.m_scale ? 1 : 4), blocks = (t.n + BLOCK8 - 1) / BLOCK8;
+        add(t.param, t.n * 4, true);
+        add(t.copy, t.n * type_bytes(t.copy_type), true);
+        add(t.m, state_bytes, true);
+        add(t.v, state_bytes, true);
+        add(t.m_scale, blocks, true);
+        add(t.v_scale, blocks, true);
+    }
+    std::sort(ranges.begin(), ranges.end(), [](const Range& x, const Range& y) { return x.first < y.first; });
+    uintptr_t end = 0, end_written = 0;                          // of the ranges in front: all, those that are written
+    for (const Range& r : ranges) {
+        if (r.first < (r.written ? end : end_written)) return true;
+        end = std::max(end, r.end);
+        if (r.written) end_written = std::max(end_written, r.end);
+    }
+    return false;
+}
+
+int64_t adamw_chunks(const atomo_adamw_tensor* tensors, int n)
+{
+    int64_t chunks = 0;
+    for (int j = 0; j < n; ++j) chunks += (tensors[j].n + CHUNK - 1) / CHUNK;
+    return chunks;
+}
+
+int adamw_create(atomo_ctx* ctx, const atomo_adamw_tensor* tensors, int n, atomo_adamw** out)
+{
+    std::vector<Tensor> table(n);
+    std::vector<Chunk> chunks, chunks8;
+    long long blocks = 0;
+    for (int j = 0; j < n; ++j) {
+        const atomo_adamw_tensor& t = tensors[j];
+        table[j] = Tensor{t.param, t.copy, t.grad, t.m, t.v, t.m_scale, t.v_scale, (long long)t.n, blocks,
+                          t.grad_type, t.copy_type, t.lr_mult, t.weight_decay};
+        blocks += (t.n + BLOCK8 - 1) / BLOCK8;
+        for (int64_t k = 0; k * CHUNK < t.n; ++k) (t.param && t.m_scale ? chunks8 : chunks).push_back(Chunk{j, (int)k});
+    }
+    std::unique_ptr<atomo_adamw> plan(new atomo_adamw());
+    plan->device = ctx->device;
+    plan->n32 = (int)chunks.size();
+    plan->n8 = (int)chunks8.size();
+    plan->updates = tensors[0].param != nullptr;
+    chunks.insert(chunks.end(), chunks8.begin(), chunks8.end());
+    const auto carve = [&](void* base) {
+        Carver c(base);
+        plan->tensors = c.take<Tensor>(n);
+        plan->chunks = c.take<Chunk>(chunks.size());
+        plan->parts = c.take<double>(NORM_PARTS);
+        return c.off;
+    };
+    if (hipMalloc(&plan->dev, carve(nullptr)) != hipSuccess) {
+        (void)hipGetLastError();
+        return ATOMO_ENOMEM;
+    }
+    carve(plan->dev);
+    hipError_t e = hipMemcpy(plan->tensors, table.data(), n * sizeof(Tensor), hipMemcpyHostToDevice);
+    if (e == hipSuccess) e = hipMemcpy(plan->chunks, chunks.data(), chunks.size() * sizeof(Chunk), hipMemcpyHostToDevice);
+    if (e == hipSuccess) e = hipDeviceSynchronize();
+    if (e != hipSuccess) {
+        ctx->last_hip = (int)e;
+        (void)hipFree(plan->dev);
+        return ATOMO_EHIP;
+    }
+    *out = plan.release();
+    return ATOMO_OK;
+}
+
+int adamw_destroy(atomo_ctx* ctx, atomo_adamw* plan)
+{
+    // (hipFree waits for the device, so no kernel still reads the tables)
+    const hipError_t e = plan->dev ? hipFree(plan->dev) : hipSuccess;
+    delete plan;
+    ATOMO_HIP(ctx, e);
+    return ATOMO_OK;
+}
+
+int adamw_device(const atomo_adamw* plan) { return plan->device; }
+bool adamw_updates(const atomo_adamw* plan) { return plan->updates; }
+
+int adamw_grad_norm(atomo_ctx* ctx, const atomo_adamw* plan, float grad_scale, float* norm, hipStream_t stream)
+{
+    ProfScope ps(ctx, ATOMO_K_ADAMW, stream);
+    const int n = plan->n32 + plan->n8, grid = std::min(n, NORM_PARTS);
+    norm_parts<<<grid, 256, 0, stream>>>(plan->tensors, plan->chunks, n, plan->parts);
+    norm_total<<<1, 256, 0, stream>>>(plan->parts, grid, fabsf(grad_scale), norm);
+    ATOMO_HIP(ctx, hipGetLastError());
+    return ATOMO_OK;
+}
+
+int adamw_step(atomo_ctx* ctx, const atomo_adamw* plan, const atomo_adamw_options& o, hipStream_t stream)
+{
+    StepArgs a = {};
+    a.lr = o.lr;
+    a.beta1 = o.beta1;
+    a.beta2 = o.beta2;
+    a.step_dev = (const long long*)o.step_dev;
+    a.lr_dev = o.lr_dev;
+    a.grad_norm = o.grad_norm;
+    a.step = o.step_dev ? 1 : o.step;
+    a.rate = o.lr / (1.0 - std::pow(o.beta1, (double)a.step));
+    a.root = (float)(1.0 / std::sqrt(1.0 - std::pow(o.beta2, (double)a.step)));
+    a.seed = o.seed;
+    a.b1 = (float)o.beta1;
+    a.c1 = (float)(1.0 - o.beta1);
+    a.b2 = (float)o.beta2;
+    a.c2 = (float)(1.0 - o.beta2);
+    a.eps = (float)o.eps;
+    a.max_norm = o.max_norm;
+    a.grad_scale = o.grad_scale;
+    ProfScope ps(ctx, ATOMO_K_ADAMW, stream);
+    if (plan->n32) adamw_states32<<<plan->n32, 256, 0, stream>>>(plan->tensors, plan->chunks, a);
+    if (plan->n8) adamw_states8<<<plan->n8, 256, 0, stream>>>(plan->tensors, plan->chunks + plan->n32, a);
+    ATOMO_HIP(ctx, hipGetLastError());
+    return ATOMO_OK;
+}
+
+int state8_unpack(atomo_ctx* ctx, int which, const uint8_t* codes, const uint8_t* scales, int64_t n, int type, void* out,
+                  hipStream_t stream)
+{
+    ProfScope ps(ctx, ATOMO_K_ADAMW, stream);
+    const unsigned grid = (unsigned)((n + 1023) / 1024);
+    with_type(type, [&](auto ty) {
+        if (which == ATOMO_STATE_V) state8_values<ty, true><<<grid, 256, 0, stream>>>(codes, scales, n, out);
+        else state8_values<ty, false><<<grid, 256, 0, stream>>>(codes, scales, n, out);
+    });
+    ATOMO_HIP(ctx, hipGetLastError());
+    return ATOMO_OK;
+}
+
+}  // namespace atomo

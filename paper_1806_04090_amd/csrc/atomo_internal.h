@@ -20,7 +20,7 @@ namespace atomo {
 // ---------------------------------------------------------------------------------------------
 
 // Device-side latched flags (int32 each).
-enum { FLAG_CAPACITY = 0, FLAG_NOCONV = 1, FLAG_MAX_SWEEPS = 2, FLAG_EIG_VISITS = 3, FLAG_EIG_INNER = 4, FLAG_DS_UPDATE_UNITS = 5, FLAG_ORDER = 6, FLAG_COUNT = 8 };
+enum { FLAG_CAPACITY = 0, FLAG_NOCONV = 1, FLAG_MAX_SWEEPS = 2, FLAG_EIG_VISITS = 3, FLAG_EIG_INNER = 4, FLAG_DS_UPDATE_UNITS = 5, FLAG_ORDER = 6, FLAG_TOKEN = 7, FLAG_COUNT = 8 };
 
 // How an SVD encode goes about a matrix: Jacobi iteration; direct encode with the iteration behind it for what that leaves
 // over; direct encode alone.
@@ -81,6 +81,8 @@ struct atomo_ctx {
     int device = 0;
     void* ws = nullptr;          // device workspace
     size_t ws_bytes = 0;
+    bool ws_in_graph = false;    // a captured call holds addresses in `ws`: it is not freed before the context
+    std::vector<void*> ws_kept;  // former workspaces of which that is so
     size_t ws_refused = SIZE_MAX;    // smallest workspace with the direct encode's part that could not be had (atomo_reserve forgets it)
     int32_t* d_flags = nullptr;  // [FLAG_COUNT] device
     int32_t* h_flags = nullptr;  // pinned readback buffer
@@ -126,6 +128,10 @@ namespace atomo {
 
 // Grows the workspace to at least `bytes` (contents are not preserved).
 int ensure_workspace(atomo_ctx* ctx, size_t bytes);
+
+// The same for work on `stream`: while that is being captured nothing is allocated (ATOMO_ENOMEM if it is too small), and
+// the block stays valid as long as the context.
+int workspace_for_stream(atomo_ctx* ctx, size_t bytes, hipStream_t stream);
 
 // Creates the context's side streams and the fork/join events if they do not exist yet.
 int ensure_side_streams(atomo_ctx* ctx);
@@ -293,5 +299,21 @@ int decode_svd_batch(atomo_ctx* ctx, const atomo_svd_msg* msgs, const int32_t* f
 int decode_entrywise(atomo_ctx* ctx, const atomo_ew_msg* msgs, int n_msgs, float scale, float* out,
                      hipStream_t stream);
 int decode_lq(atomo_ctx* ctx, const atomo_lq_msg* msgs, int n_msgs, float scale, float* out, hipStream_t stream);
+
+size_t embedding_workspace_bytes(int64_t n_tokens, int64_t rows, int32_t cols);
+int embedding(atomo_ctx* ctx, const atomo_rows& table, const atomo_tokens& tokens, float scale, const atomo_rows& out, hipStream_t stream);
+int embedding_grad(atomo_ctx* ctx, const atomo_tokens& tokens, const atomo_rows& dy, float scale, const atomo_rows& grad,
+                   bool accumulate, hipStream_t stream);
+
+bool adamw_overlap(const atomo_adamw_tensor* tensors, int n);
+int64_t adamw_chunks(const atomo_adamw_tensor* tensors, int n);
+int adamw_create(atomo_ctx* ctx, const atomo_adamw_tensor* tensors, int n, atomo_adamw** out);
+int adamw_destroy(atomo_ctx* ctx, atomo_adamw* plan);
+int adamw_device(const atomo_adamw* plan);
+bool adamw_updates(const atomo_adamw* plan);     // false: a plan of gradients alone
+int adamw_grad_norm(atomo_ctx* ctx, const atomo_adamw* plan, float grad_scale, float* norm, hipStream_t stream);
+int adamw_step(atomo_ctx* ctx, const atomo_adamw* plan, const atomo_adamw_options& opt, hipStream_t stream);
+int state8_unpack(atomo_ctx* ctx, int which, const uint8_t* codes, const uint8_t* scales, int64_t n, int type, void* out,
+                  hipStream_t stream);
 
 }  // namespace atomo

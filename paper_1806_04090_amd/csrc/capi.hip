@@ -4,16 +4,18 @@
 #include <cstring>
 #include <new>
 
-#include "atomo_internal.h"
+#include "element_types.h"
 
 namespace atomo {
 
 int ensure_workspace(atomo_ctx* ctx, size_t bytes)
 {
     if (bytes <= ctx->ws_bytes) return ATOMO_OK;
-    // Growing frees the old block; hipFree waits for the device, so no kernel still uses it.
+    // Growing frees the old block (hipFree waits for the device, so no kernel still uses it), unless a graph may run on it again.
     if (ctx->ws) {
-        ATOMO_HIP(ctx, hipFree(ctx->ws));
+        if (ctx->ws_in_graph) ctx->ws_kept.push_back(ctx->ws);
+        else ATOMO_HIP(ctx, hipFree(ctx->ws));
+        ctx->ws_in_graph = false;
         ctx->ws = nullptr;
         ctx->ws_bytes = 0;
     }
@@ -26,6 +28,16 @@ int ensure_workspace(atomo_ctx* ctx, size_t bytes)
         return ATOMO_ENOMEM;
     }
     ctx->ws_bytes = want;
+    return ATOMO_OK;
+}
+
+int workspace_for_stream(atomo_ctx* ctx, size_t bytes, hipStream_t stream)
+{
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    ATOMO_HIP(ctx, hipStreamIsCapturing(stream, &capture));
+    if (capture == hipStreamCaptureStatusNone) return ensure_workspace(ctx, bytes);
+    if (bytes > ctx->ws_bytes) return ATOMO_ENOMEM;
+    ctx->ws_in_graph = true;
     return ATOMO_OK;
 }
 
@@ -189,6 +201,7 @@ int atomo_destroy(atomo_ctx* ctx)
     if (ctx->side2) (void)hipStreamDestroy(ctx->side2);
     if (ctx->side_thin) (void)hipStreamDestroy(ctx->side_thin);
     if (ctx->ws) (void)hipFree(ctx->ws);
+    for (void* kept : ctx->ws_kept) (void)hipFree(kept);
     for (TableCache* cache : {&ctx->svd_tables, &ctx->dec_tables, &ctx->prob_tables})
         for (TableSlot& t : cache->slot)
             if (t.dev) (void)hipFree(t.dev);
@@ -206,7 +219,7 @@ int atomo_reserve(atomo_ctx* ctx, size_t bytes)
     DeviceGuard guard(ctx);
     if (!guard.ok) return ATOMO_EHIP;
     ctx->ws_refused = SIZE_MAX;
-    return ensure_workspace(ctx, bytes);
+    return guarded([&] { return ensure_workspace(ctx, bytes); });
 }
 
 int atomo_svd_workspace_bytes(const atomo_mat* mats, int n_mats, size_t* bytes)
@@ -234,7 +247,7 @@ int atomo_status(atomo_ctx* ctx, void* stream, int32_t* sweeps)
     if (sweeps) *sweeps = ctx->h_flags[FLAG_MAX_SWEEPS];
     if (ctx->h_flags[FLAG_CAPACITY]) return ATOMO_ECAPACITY;
     if (ctx->h_flags[FLAG_NOCONV]) return ATOMO_ENOCONV;
-    if (ctx->h_flags[FLAG_ORDER]) return ATOMO_EINVAL;
+    if (ctx->h_flags[FLAG_ORDER] || ctx->h_flags[FLAG_TOKEN]) return ATOMO_EINVAL;
     return ATOMO_OK;
 }
 
@@ -309,7 +322,7 @@ int atomo_measure_mfma_fp32(atomo_ctx* ctx, double* tflops, void* stream)
     DeviceGuard guard(ctx);
     if (!guard.ok) return ATOMO_EHIP;
     hipStream_t st = (hipStream_t)stream;
-    int rc = ensure_workspace(ctx, 256);
+    int rc = guarded([&] { return ensure_workspace(ctx, 256); });
     if (rc != ATOMO_OK) return rc;
     hipDeviceProp_t prop;
     ATOMO_HIP(ctx, hipGetDeviceProperties(&prop, ctx->device));
@@ -498,6 +511,113 @@ int atomo_decode(atomo_ctx* ctx, int kind, const void* msgs, int n_msgs, float s
         return guarded([&] { return decode_lq(ctx, m, n_msgs, scale, out, (hipStream_t)stream); });
     }
     return ATOMO_EINVAL;
+}
+
+namespace {
+
+bool bad_rows(const atomo_rows& m, bool written, bool may_be_empty)
+{
+    if (m.rows < (may_be_empty ? 0 : 1) || m.rows >= INT32_MAX || m.cols < 1 || !known_type(m.type)) return true;
+    if (m.rows > 0 && !m.data) return true;
+    return m.rows > 1 && (written || m.ld != 0) && m.ld < m.cols;
+}
+
+bool bad_tokens(const atomo_tokens& t)
+{
+    return t.n < 0 || t.n > INT32_MAX || (t.bytes != 4 && t.bytes != 8) || (t.n > 0 && !t.data);
+}
+
+bool finite_not_negative(double x) { return x >= 0.0 && !std::isinf(x); }
+
+}  // namespace
+
+int atomo_embedding(atomo_ctx* ctx, const atomo_rows* table, const atomo_tokens* tokens, float scale, const atomo_rows* out,
+                    void* stream)
+{
+    if (!ctx || !table || !tokens || !out || bad_rows(*table, false, false) || bad_tokens(*tokens) || bad_rows(*out, true, true))
+        return ATOMO_EINVAL;
+    if (out->cols != table->cols || out->rows < tokens->n) return ATOMO_EINVAL;
+    DeviceGuard guard(ctx);
+    if (!guard.ok) return ATOMO_EHIP;
+    return guarded([&] { return embedding(ctx, *table, *tokens, scale, *out, (hipStream_t)stream); });
+}
+
+int atomo_embedding_grad(atomo_ctx* ctx, const atomo_tokens* tokens, const atomo_rows* dy, float scale, const atomo_rows* grad,
+                         int accumulate, void* stream)
+{
+    if (!ctx || !tokens || !dy || !grad || bad_tokens(*tokens) || bad_rows(*dy, false, true) || bad_rows(*grad, true, false))
+        return ATOMO_EINVAL;
+    if (dy->cols != grad->cols || dy->rows < tokens->n) return ATOMO_EINVAL;
+    DeviceGuard guard(ctx);
+    if (!guard.ok) return ATOMO_EHIP;
+    return guarded([&] { return embedding_grad(ctx, *tokens, *dy, scale, *grad, accumulate != 0, (hipStream_t)stream); });
+}
+
+int atomo_embedding_workspace_bytes(int64_t n_tokens, int64_t rows, int32_t cols, size_t* bytes)
+{
+    if (n_tokens < 0 || n_tokens > INT32_MAX || rows < 1 || rows >= INT32_MAX || cols < 1 || !bytes) return ATOMO_EINVAL;
+    *bytes = embedding_workspace_bytes(n_tokens, rows, cols);
+    return ATOMO_OK;
+}
+
+int atomo_adamw_create(atomo_ctx* ctx, const atomo_adamw_tensor* tensors, int n, atomo_adamw** out)
+{
+    if (!out) return ATOMO_EINVAL;
+    *out = nullptr;
+    if (!ctx || !tensors || n <= 0) return ATOMO_EINVAL;
+    for (int j = 0; j < n; ++j) {
+        const atomo_adamw_tensor& t = tensors[j];
+        if (t.n <= 0 || t.n >= ((int64_t)1 << 40) || !t.grad || !known_type(t.grad_type)) return ATOMO_EINVAL;
+        if (!t.param != !tensors[0].param) return ATOMO_EINVAL;
+        if (!t.param) continue;
+        if (!t.m || !t.v || !t.m_scale != !t.v_scale || (t.copy && !known_type(t.copy_type))) return ATOMO_EINVAL;
+        if (!finite_not_negative(t.lr_mult) || !finite_not_negative(t.weight_decay)) return ATOMO_EINVAL;
+    }
+    if (adamw_chunks(tensors, n) >= 1 << 24) return ATOMO_EINVAL;                // (a grid has less than 2^32 threads)
+    return guarded([&] {
+        if (adamw_overlap(tensors, n)) return (int)ATOMO_EINVAL;
+        DeviceGuard guard(ctx);
+        if (!guard.ok) return (int)ATOMO_EHIP;
+        return adamw_create(ctx, tensors, n, out);
+    });
+}
+
+int atomo_adamw_destroy(atomo_ctx* ctx, atomo_adamw* plan)
+{
+    if (!ctx || !plan || adamw_device(plan) != ctx->device) return ATOMO_EINVAL;
+    DeviceGuard guard(ctx);
+    if (!guard.ok) return ATOMO_EHIP;
+    return adamw_destroy(ctx, plan);
+}
+
+int atomo_adamw_grad_norm(atomo_ctx* ctx, const atomo_adamw* plan, float grad_scale, float* norm, void* stream)
+{
+    if (!ctx || !plan || !norm || !std::isfinite(grad_scale) || adamw_device(plan) != ctx->device) return ATOMO_EINVAL;
+    DeviceGuard guard(ctx);
+    if (!guard.ok) return ATOMO_EHIP;
+    return guarded([&] { return adamw_grad_norm(ctx, plan, grad_scale, norm, (hipStream_t)stream); });
+}
+
+int atomo_adamw_step(atomo_ctx* ctx, const atomo_adamw* plan, const atomo_adamw_options* opt, void* stream)
+{
+    if (!ctx || !plan || !opt || adamw_device(plan) != ctx->device || !adamw_updates(plan)) return ATOMO_EINVAL;
+    const auto bad_beta = [](double b) { return !(b >= 0.0 && b < 1.0); };
+    if (bad_beta(opt->beta1) || bad_beta(opt->beta2) || !finite_not_negative(opt->eps) || !finite_not_negative(opt->lr)) return ATOMO_EINVAL;
+    if (!opt->step_dev && opt->step < 1) return ATOMO_EINVAL;
+    if (!finite_not_negative(opt->max_norm) || (opt->max_norm > 0.0f && !opt->grad_norm) || !std::isfinite(opt->grad_scale)) return ATOMO_EINVAL;
+    DeviceGuard guard(ctx);
+    if (!guard.ok) return ATOMO_EHIP;
+    return guarded([&] { return adamw_step(ctx, plan, *opt, (hipStream_t)stream); });
+}
+
+int atomo_state8_unpack(atomo_ctx* ctx, int which, const uint8_t* codes, const uint8_t* scales, int64_t n, int type, void* out,
+                        void* stream)
+{
+    if (!ctx || !codes || !scales || !out || n <= 0 || n >= ((int64_t)1 << 34) || !known_type(type)) return ATOMO_EINVAL;
+    if (which != ATOMO_STATE_M && which != ATOMO_STATE_V) return ATOMO_EINVAL;
+    DeviceGuard guard(ctx);
+    if (!guard.ok) return ATOMO_EHIP;
+    return guarded([&] { return state8_unpack(ctx, which, codes, scales, n, type, out, (hipStream_t)stream); });
 }
 
 }  // extern "C"
