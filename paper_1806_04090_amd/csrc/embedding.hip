@@ -62,120 +62,156 @@ __global__ __launch_bounds__(256) void embedding_rows(Tokens tokens, const void*
 }
 
 // ---------------------------------------------------------------------------------------------
-// Sort: least significant digit first, three launches per digit
+// Sort
 // ---------------------------------------------------------------------------------------------
 
-constexpr int MOST_BINS = 1024, MOST_PARTS = 512;
-
-struct Digit { int shift, bits; };
-
-// Keys of the first pass come from the tokens themselves: their rows, `rows` for those that have none.
-__device__ inline uint32_t key_at(const Tokens& t, const uint32_t* keys, int i, int rows, int32_t* flags)
+// The key of a token: its row, or `rows` if it has none.
+__device__ inline uint32_t key_of_token(const Tokens& t, long long i, int rows, int32_t* flags)
 {
-    if (keys) return keys[i];
     const int row = row_of(t, i, rows);
     if (row == -2 && flags) flags[FLAG_TOKEN] = 1;
     return row < 0 ? (uint32_t)rows : (uint32_t)row;
 }
 
-// counts[digit][part]
-__global__ __launch_bounds__(256) void sort_count(Tokens tokens, const uint32_t* keys, int rows, Digit d, int per, int* counts, int32_t* flags)
+// Few tokens: the place of each is the number of those in front of it, by comparison with all.  One launch; n^2 comparisons.
+// A workgroup has 64 tokens, one per lane of each of its sixteen waves, which share the keys to compare with.
+constexpr int RANKED = 8192;
+
+__global__ __launch_bounds__(1024) void sort_by_rank(Tokens tokens, int rows, uint32_t* keys_out, uint32_t* from_out, int32_t* flags)
+{
+    __shared__ uint32_t keys[RANKED];
+    __shared__ int ranks[16][64];
+    const int n = tokens.n, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int blocks = (n + 63) / 64, own = blockIdx.x;
+    for (int i = threadIdx.x; i < blocks * 64; i += 1024) keys[i] = i < n ? key_of_token(tokens, i, rows, flags) : 0xffffffffu;
+    __syncthreads();
+    const uint32_t key = keys[own * 64 + lane];
+    int rank = 0;
+    for (int b = wave; b < blocks; b += 16) {
+        const uint32_t* const other = keys + b * 64;
+        // (key, place) in front of (this key, this place); behind the own block equal keys are not
+        const uint32_t limit = b < own ? key + 1 : key;          // (keys are below 2^31)
+#pragma unroll 16
+        for (int j = 0; j < 64; ++j) rank += other[j] < limit ? 1 : 0;
+        if (b == own) {
+            for (int j = 0; j < 64; ++j) rank += other[j] == key && j < lane ? 1 : 0;
+        }
+    }
+    ranks[wave][lane] = rank;
+    __syncthreads();
+    if (wave == 0 && own * 64 + lane < n) {
+        int to = 0;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) to += ranks[w][lane];
+        keys_out[to] = key;
+        from_out[to] = (uint32_t)(own * 64 + lane);
+    }
+}
+
+// More: least significant digit first, two launches per digit.  A workgroup of sixteen waves has a part of the keys; few parts, so that each
+// can add up the counts of those in front of it by itself.
+constexpr int MOST_BITS = 9, MOST_BINS = 1 << MOST_BITS;
+constexpr int ROUNDS = 4;              // keys of a lane that are on their way at a time
+
+struct Digit { int shift, bits; };
+
+__device__ inline uint32_t key_at(const Tokens& t, const uint32_t* keys, long long i, int rows, int32_t* flags)
+{
+    return keys ? keys[i] : key_of_token(t, i, rows, flags);
+}
+
+// counts[part][digit]
+__global__ __launch_bounds__(1024) void sort_count(Tokens tokens, const uint32_t* keys, int rows, Digit d, int per, int* counts, int32_t* flags)
 {
     __shared__ int hist[MOST_BINS];
     const int bins = 1 << d.bits;
-    for (int b = threadIdx.x; b < bins; b += 256) hist[b] = 0;
+    if ((int)threadIdx.x < bins) hist[threadIdx.x] = 0;
     __syncthreads();
-    const long long first = (long long)blockIdx.x * per;
-    for (int i = threadIdx.x; i < per && first + i < tokens.n; i += 256)
-        atomicAdd(&hist[key_at(tokens, keys, (int)(first + i), rows, flags) >> d.shift & (bins - 1)], 1);
+    const long long first = (long long)blockIdx.x * per, end = min(first + per, (long long)tokens.n);
+    for (long long i = first + threadIdx.x; i < end; i += 1024) atomicAdd(&hist[key_at(tokens, keys, i, rows, flags) >> d.shift & (bins - 1)], 1);
     __syncthreads();
-    for (int b = threadIdx.x; b < bins; b += 256) counts[(long long)b * gridDim.x + blockIdx.x] = hist[b];
+    if ((int)threadIdx.x < bins) counts[(long long)blockIdx.x * bins + threadIdx.x] = hist[threadIdx.x];
 }
 
-// One wave per digit: counts in front of each part, and the total.
-__global__ __launch_bounds__(64) void sort_sums(int* counts, int parts, int* totals)
-{
-    int* const c = counts + (long long)blockIdx.x * parts;
-    int before = 0;
-    for (int base = 0; base < parts; base += 64) {
-        const int i = base + (int)threadIdx.x;
-        const int own = i < parts ? c[i] : 0;
-        int sum = own;
-#pragma unroll
-        for (int s = 1; s < 64; s <<= 1) {
-            const int other = __shfl_up(sum, s);
-            if ((int)threadIdx.x >= s) sum += other;
-        }
-        if (i < parts) c[i] = before + sum - own;
-        before += __shfl(sum, 63);
-    }
-    if (threadIdx.x == 0) totals[blockIdx.x] = before;
-}
-
-// Each wave takes a quarter of the part, 64 keys after the other: a key's place is that of its digit, plus what the waves in front and the
+// Each wave takes a sixteenth of the part, 64 keys after the other: a key's place is that of its digit, plus what the waves in front and the
 // keys in front of it have of the same digit.
-__global__ __launch_bounds__(256) void sort_place(Tokens tokens, const uint32_t* keys, const uint32_t* from, int rows, Digit d, int per,
-                                                  const int* counts, const int* totals, uint32_t* keys_out, uint32_t* from_out)
+__global__ __launch_bounds__(1024) void sort_place(Tokens tokens, const uint32_t* keys, const uint32_t* from, int rows, Digit d, int per,
+                                                   int parts, const int* counts, uint32_t* keys_out, uint32_t* from_out)
 {
-    __shared__ int at[4][MOST_BINS];
-    __shared__ int sums[256];
+    __shared__ int at[16][MOST_BINS];
+    __shared__ int sums[8];
     const int bins = 1 << d.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int b = threadIdx.x; b < bins; b += 256)
-        for (int w = 0; w < 4; ++w) at[w][b] = 0;
+    for (int b = threadIdx.x; b < 16 * MOST_BINS; b += 1024) ((int*)at)[b] = 0;
     __syncthreads();
-    const long long first = (long long)blockIdx.x * per + wave * (per / 4);
-    const long long end = min(first + per / 4, (long long)tokens.n);
-    for (long long i = first + lane; i < end; i += 64)
-        atomicAdd(&at[wave][key_at(tokens, keys, (int)i, rows, nullptr) >> d.shift & (bins - 1)], 1);
-    // places of the digits: sums over the totals in front
-    const int share = (bins + 255) / 256;
-    int own = 0;
-    for (int k = 0; k < share; ++k) {
-        const int b = threadIdx.x * share + k;
-        if (b < bins) own += totals[b];
+    const long long first = (long long)blockIdx.x * per + wave * (per / 16);
+    const long long end = min(first + per / 16, (long long)tokens.n);
+    for (long long base = first; base < end; base += 64 * ROUNDS) {
+        uint32_t key[ROUNDS];
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const long long i = base + r * 64 + lane;
+            key[r] = i < end ? key_at(tokens, keys, i, rows, nullptr) : 0;
+        }
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r)
+            if (base + r * 64 + lane < end) atomicAdd(&at[wave][key[r] >> d.shift & (bins - 1)], 1);
     }
-    sums[threadIdx.x] = own;
+    // a thread per digit: how often it comes in the parts in front, and at all
+    int before = 0, total = 0;
+    if ((int)threadIdx.x < bins) {
+#pragma unroll 16
+        for (int p = 0; p < parts; ++p) {
+            const int c = counts[(long long)p * bins + threadIdx.x];
+            total += c;
+            before += p < (int)blockIdx.x ? c : 0;
+        }
+    }
+    int sum = total;                                             // of the digits up to this one, first within the wave
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const int other = __shfl_up(sum, s);
+        if (lane >= s) sum += other;
+    }
+    if (wave < 8 && lane == 63) sums[wave] = sum;
     __syncthreads();
-    for (int s = 1; s < 256; s <<= 1) {
-        const int other = (int)threadIdx.x >= s ? sums[threadIdx.x - s] : 0;
-        __syncthreads();
-        sums[threadIdx.x] += other;
-        __syncthreads();
+    if ((int)threadIdx.x < bins) {
+        int place = before + sum - total;
+        for (int w = 0; w < wave; ++w) place += sums[w];
+#pragma unroll
+        for (int w = 0; w < 16; ++w) {
+            const int c = at[w][threadIdx.x];
+            at[w][threadIdx.x] = place;
+            place += c;
+        }
     }
-    int place = sums[threadIdx.x] - own;
-    for (int k = 0; k < share; ++k) {
-        const int b = threadIdx.x * share + k;
-        if (b < bins) {
-            int p = place + counts[(long long)b * gridDim.x + blockIdx.x];
-            place += totals[b];
-            for (int w = 0; w < 4; ++w) {
-                const int n = at[w][b];
-                at[w][b] = p;
-                p += n;
+    __syncthreads();
+    for (long long base = first; base < end; base += 64 * ROUNDS) {
+        uint32_t key[ROUNDS], source[ROUNDS];
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const long long i = base + r * 64 + lane;
+            key[r] = i < end ? key_at(tokens, keys, i, rows, nullptr) : 0;
+            source[r] = i < end && from ? from[i] : (uint32_t)i;
+        }
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const bool live = base + r * 64 + lane < end;
+            const int digit = (int)(key[r] >> d.shift & (bins - 1));
+            uint64_t same = __ballot(live);
+            for (int b = 0; b < d.bits; ++b) {
+                const uint64_t set = __ballot(digit >> b & 1);
+                same &= (digit >> b & 1) ? set : ~set;
             }
-        }
-    }
-    __syncthreads();
-    for (long long base = first; base < end; base += 64) {
-        const long long i = base + lane;
-        const bool live = i < end;
-        const uint32_t key = live ? key_at(tokens, keys, (int)i, rows, nullptr) : 0;
-        const uint32_t source = live ? (from ? from[i] : (uint32_t)i) : 0;
-        const int digit = (int)(key >> d.shift & (bins - 1));
-        uint64_t same = __ballot(live);
-        for (int b = 0; b < d.bits; ++b) {
-            const uint64_t set = __ballot(digit >> b & 1);
-            same &= (digit >> b & 1) ? set : ~set;
-        }
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        int to = 0;
-        if (live) to = at[wave][digit] + rank;
-        lanes_in_order();
-        if (live && rank == 0) at[wave][digit] += __popcll(same);
-        lanes_in_order();
-        if (live) {
-            keys_out[to] = key;
-            from_out[to] = source;
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            int to = 0;
+            if (live) to = at[wave][digit] + rank;
+            lanes_in_order();
+            if (live && rank == 0) at[wave][digit] += __popcll(same);
+            lanes_in_order();
+            if (live) {
+                keys_out[to] = key[r];
+                from_out[to] = source[r];
+            }
         }
     }
 }
@@ -251,20 +287,25 @@ struct Grad {
     uint32_t rows;
     int cols;
     float scale;
-    int accumulate;
 };
 
+// `before`: what the row held, if sums are added to it.  Lanes that overlap have all read that before one of them writes.
 template <int OUT, int VEC>
-__device__ inline void write_sum(const Grad& g, uint32_t row, int col, Cols<VEC> sum)
+__device__ inline Cols<VEC> load_before(const Grad& g, uint32_t row, int col)
 {
-    const long long at = (long long)row * g.ld + col;
+    return load_cols<OUT, VEC>(g.data, (long long)row * g.ld + col);
+}
+
+template <int OUT, bool ACC, int VEC>
+__device__ inline void write_sum(const Grad& g, uint32_t row, int col, Cols<VEC> sum, const Cols<VEC>& before)
+{
 #pragma unroll
     for (int k = 0; k < VEC; ++k) sum.x[k] *= g.scale;
-    if (g.accumulate) {
-        add(sum, load_cols<OUT, VEC>(g.data, at));
-        lanes_in_order();                                        // (lanes that overlap have all read before one writes)
+    if constexpr (ACC) {
+        add(sum, before);
+        lanes_in_order();
     }
-    store_cols<OUT, VEC>(g.data, at, sum);
+    store_cols<OUT, VEC>(g.data, (long long)row * g.ld + col, sum);
 }
 
 // Sums of the runs of equal keys among PIECE sorted tokens, by one wave: runs that lie within the piece are written, the
@@ -280,29 +321,35 @@ struct Pieces {
 
 constexpr int AHEAD = 8;               // rows on their way at a time
 
-template <int IN, int OUT, int VEC>
+template <int IN, int OUT, int VEC, bool ACC>
 __device__ void sum_piece(const Pieces& s, int piece, const void* dy, long long ld_dy, int col, bool mine, const Grad& g)
 {
     const int lane = threadIdx.x & 63, first = piece * s.length;
     const int here = min(s.length, s.n - first);
     const uint32_t key = lane < here ? s.keys[first + lane] : g.rows;
     const uint32_t from = lane < here ? s.from[first + lane] : 0;
+    const uint32_t in_front = first > 0 ? s.keys[first - 1] : g.rows, behind = first + s.length < s.n ? s.keys[first + s.length] : g.rows;
     const int count = __popcll(__ballot(key < g.rows));          // (those of no row stand behind all others)
     if (count == 0) return;
-    const bool begun = first > 0 && s.keys[first - 1] == (uint32_t)__builtin_amdgcn_readfirstlane((int)key);
-    const uint32_t last = (uint32_t)__builtin_amdgcn_readlane((int)key, count - 1);
-    const bool goes_on = count == s.length && first + count < s.n && s.keys[first + count] == last;
+    const bool begun = in_front == (uint32_t)__builtin_amdgcn_readfirstlane((int)key);
+    const bool goes_on = count == s.length && behind == (uint32_t)__builtin_amdgcn_readlane((int)key, count - 1);
     const uint32_t next = (uint32_t)__shfl_down((int)key, 1);
     const uint64_t ends = __ballot(lane < count && (lane == count - 1 || key != next));
     Cols<VEC> sum = {};
     bool in_first = true;
     for (int i = 0; i < count; i += AHEAD) {
-        Cols<VEC> x[AHEAD];
+        Cols<VEC> x[AHEAD], before[ACC ? AHEAD : 1];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
             if (i + u < count) {
                 const long long row = (long long)(uint32_t)__builtin_amdgcn_readlane((int)from, i + u);
-                if (mine) x[u] = load_cols<IN, VEC>(dy, row * ld_dy + col);
+                const uint32_t to = (uint32_t)__builtin_amdgcn_readlane((int)key, i + u);
+                if (mine) {
+                    x[u] = load_cols<IN, VEC>(dy, row * ld_dy + col);
+                    if constexpr (ACC) {
+                        if (ends >> (i + u) & 1) before[u] = load_before<OUT, VEC>(g, to, col);
+                    }
+                }
             }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
@@ -313,7 +360,7 @@ __device__ void sum_piece(const Pieces& s, int piece, const void* dy, long long 
                     if (mine) {
                         if (in_first && begun) store_cols<ATOMO_F32, VEC>(s.heads, piece * s.ld + col, sum);
                         else if (i + u == count - 1 && goes_on) store_cols<ATOMO_F32, VEC>(s.tails, piece * s.ld + col, sum);
-                        else write_sum<OUT, VEC>(g, row, col, sum);
+                        else write_sum<OUT, ACC, VEC>(g, row, col, sum, before[ACC ? u : 0]);
                     }
                     in_first = false;
                     sum = Cols<VEC>{};
@@ -337,6 +384,22 @@ __device__ inline int keys_below(const uint32_t* keys, int n, uint32_t key)
 }
 
 constexpr int ZERO_ROWS = 256;         // most rows of a workgroup that writes zeros
+
+// Zeros in those of the rows [first, end) that are not named, a wave per row.
+template <int OUT>
+__device__ inline void write_zeros(const uint8_t* named, uint32_t first, uint32_t end, const Grad& g)
+{
+    constexpr int VEC = OUT == ATOMO_F32 ? 4 : 8;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const Cols<VEC> zero = {};
+    for (uint32_t r = first + wave; r < end; r += 4) {
+        if (named[r - first]) continue;
+        for (int col = lane * VEC; col < g.cols; col += 64 * VEC) {
+            if (col + VEC <= g.cols) store_cols<OUT, VEC>(g.data, (long long)r * g.ld + col, zero);
+            else for (int j = col; j < g.cols; ++j) store1<OUT>(g.data, (long long)r * g.ld + j, 0.0f);
+        }
+    }
+}
 
 // Zeros for those of `per` rows that no token names.
 template <int OUT>
@@ -363,19 +426,11 @@ __device__ void zero_rows(const uint32_t* keys, int n, uint32_t first, int per, 
         named[threadIdx.x] = lo < hi && keys[lo] == row;
     }
     __syncthreads();
-    constexpr int VEC = OUT == ATOMO_F32 ? 4 : 8;
-    const Cols<VEC> zero = {};
-    for (uint32_t r = first + wave; r < end; r += 4) {
-        if (named[r - first]) continue;
-        for (int col = lane * VEC; col < g.cols; col += 64 * VEC) {
-            if (col + VEC <= g.cols) store_cols<OUT, VEC>(g.data, (long long)r * g.ld + col, zero);
-            else for (int j = col; j < g.cols; ++j) store1<OUT>(g.data, (long long)r * g.ld + j, 0.0f);
-        }
-    }
+    write_zeros<OUT>(named, first, end, g);
 }
 
 // Waves of the first workgroups take a piece and a tile of columns each; the workgroups behind them write the zeros.
-template <int IN, int OUT, int VEC>
+template <int IN, int OUT, int VEC, bool ACC>
 __global__ __launch_bounds__(256) void sum_pieces(Pieces s, const void* dy, long long ld_dy, Grad g, int pieces, int tiles, unsigned groups, int zero_per)
 {
     if (blockIdx.x >= groups) {
@@ -389,16 +444,31 @@ __global__ __launch_bounds__(256) void sum_pieces(Pieces s, const void* dy, long
     for (long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); w < (long long)pieces * tiles; w += (long long)groups * 4) {
         const int piece = __builtin_amdgcn_readfirstlane((int)(w / tiles)), tile = __builtin_amdgcn_readfirstlane((int)(w % tiles));
         const int first = tile * (64 * VEC), left = g.cols - first;
-        if (left >= VEC) sum_piece<IN, OUT, VEC>(s, piece, dy, ld_dy, min(first + lane * VEC, g.cols - VEC), lane * VEC < left, g);
-        else sum_piece<IN, OUT, 1>(s, piece, dy, ld_dy, first + lane, lane < left, g);
+        if (left >= VEC) sum_piece<IN, OUT, VEC, ACC>(s, piece, dy, ld_dy, min(first + lane * VEC, g.cols - VEC), lane * VEC < left, g);
+        else sum_piece<IN, OUT, 1, ACC>(s, piece, dy, ld_dy, first + lane, lane < left, g);
     }
 }
 
 // Runs over several pieces: the tail of the piece in which a run begins, and the heads of those behind it up to its end.  A
-// workgroup looks after 64 pieces and 256 columns; a wave adds up to SHORT rows by itself, longer runs are shared out among the sixteen.
-constexpr int SHORT = 16;
+// workgroup looks after JOINED pieces and 256 columns; a wave adds up to SHORT rows by itself, longer runs are shared out among the sixteen.
+constexpr int SHORT = 16, JOINED = 16;
 
-template <int OUT, int VEC>
+// The sum of rows [k, end), AHEAD of them on their way at a time.
+template <int VEC>
+__device__ inline void add_rows(Cols<VEC>& sum, const float* rows, long long ld, int k, int end, int col)
+{
+    for (; k < end; k += AHEAD) {
+        Cols<VEC> x[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (k + u < end) x[u] = load_cols<ATOMO_F32, VEC>(rows, (k + u) * ld + col);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (k + u < end) add(sum, x[u]);
+    }
+}
+
+template <int OUT, int VEC, bool ACC>
 __device__ void join_tile(const Pieces& s, int pieces, int base, int col, bool mine, const Grad& g)
 {
     __shared__ Cols<VEC> part[16][64];
@@ -408,18 +478,13 @@ __device__ void join_tile(const Pieces& s, int pieces, int base, int col, bool m
     int last = 0;
     uint32_t key = g.rows;
     const long long end = (long long)(piece + 1) * s.length;
-    if (piece < pieces && end < s.n) {
+    if (lane < JOINED && piece < pieces && end < s.n) {
         key = s.keys[end - 1];
-        const bool begins = s.keys[end - s.length] != key || piece == 0 || s.keys[end - s.length - 1] != key;
-        if (key < g.rows && begins && s.keys[end] == key) {
-            int step = 1;                                        // the last piece whose first key is this one
-            last = piece + 1;
-            while (last + step < pieces && s.keys[(long long)(last + step) * s.length] == key) {
-                last += step;
-                step *= 2;
-            }
-            for (; step > 0; step /= 2)
-                if (last + step < pieces && s.keys[(long long)(last + step) * s.length] == key) last += step;
+        const uint32_t first = s.keys[end - s.length], in_front = piece ? s.keys[end - s.length - 1] : g.rows, behind = s.keys[end];
+        if (key < g.rows && (first != key || in_front != key) && behind == key) {
+            last = piece + 1;                                    // the pieces behind whose first key is this one
+#pragma unroll
+            for (int k = 1; k <= SHORT; ++k) last += piece + 1 + k < pieces && s.keys[end + (long long)k * s.length] == key ? 1 : 0;
         }
     }
     const uint64_t runs = __ballot(last > 0), longer = __ballot(last - piece > SHORT && last > 0);
@@ -429,41 +494,132 @@ __device__ void join_tile(const Pieces& s, int pieces, int base, int col, bool m
         const int p = base + at, q = __builtin_amdgcn_readlane(last, at);
         const uint32_t row = (uint32_t)__builtin_amdgcn_readlane((int)key, at);
         if (turn % 16 != wave || !mine) continue;
-        Cols<VEC> sum = load_cols<ATOMO_F32, VEC>(s.tails, p * s.ld + col);
-#pragma unroll 4
-        for (int k = p + 1; k <= q; ++k) add(sum, load_cols<ATOMO_F32, VEC>(s.heads, k * s.ld + col));
-        write_sum<OUT, VEC>(g, row, col, sum);
+        Cols<VEC> before = {}, sum;
+        if constexpr (ACC) before = load_before<OUT, VEC>(g, row, col);
+        sum = load_cols<ATOMO_F32, VEC>(s.tails, p * s.ld + col);
+        add_rows(sum, s.heads, s.ld, p + 1, q + 1, col);
+        write_sum<OUT, ACC, VEC>(g, row, col, sum, before);
     }
     for (uint64_t left = longer; left; left &= left - 1) {
         const int at = __builtin_ctzll(left);
-        const int p = base + at, q = __builtin_amdgcn_readlane(last, at), share = (q - p + 15) / 16;
         const uint32_t row = (uint32_t)__builtin_amdgcn_readlane((int)key, at);
+        const int p = base + at, q = (keys_below(s.keys, s.n, row + 1) - 1) / s.length, share = (q - p + 15) / 16;
         const int k0 = p + 1 + wave * share, k1 = min(k0 + share, q + 1);
-        Cols<VEC> sum = {};
-        if (mine) {
-#pragma unroll 8
-            for (int k = k0; k < k1; ++k) add(sum, load_cols<ATOMO_F32, VEC>(s.heads, k * s.ld + col));
-        }
+        Cols<VEC> sum = {}, before = {};
+        if (mine) add_rows(sum, s.heads, s.ld, k0, k1, col);
         part[wave][lane] = sum;
+        if (wave == 0 && mine) {
+            if constexpr (ACC) before = load_before<OUT, VEC>(g, row, col);
+            sum = load_cols<ATOMO_F32, VEC>(s.tails, p * s.ld + col);
+        }
         __syncthreads();
         if (wave == 0 && mine) {
-            sum = load_cols<ATOMO_F32, VEC>(s.tails, p * s.ld + col);
 #pragma unroll
             for (int w = 0; w < 16; ++w) add(sum, part[w][lane]);
-            write_sum<OUT, VEC>(g, row, col, sum);
+            write_sum<OUT, ACC, VEC>(g, row, col, sum, before);
         }
         __syncthreads();
     }
 }
 
-template <int OUT>
+template <int OUT, bool ACC>
 __global__ __launch_bounds__(1024) void join_pieces(Pieces s, Grad g, int pieces)
 {
     const int lane = threadIdx.x & 63;
     for (int tile = blockIdx.y; tile * 256 < g.cols; tile += gridDim.y) {
         const int first = tile * 256, left = g.cols - first;
-        if (left >= 4) join_tile<OUT, 4>(s, pieces, (int)blockIdx.x * 64, min(first + lane * 4, g.cols - 4), lane * 4 < left, g);
-        else join_tile<OUT, 1>(s, pieces, (int)blockIdx.x * 64, first + lane, lane < left, g);
+        if (left >= 4) join_tile<OUT, 4, ACC>(s, pieces, (int)blockIdx.x * JOINED, min(first + lane * 4, g.cols - 4), lane * 4 < left, g);
+        else join_tile<OUT, 1, ACC>(s, pieces, (int)blockIdx.x * JOINED, first + lane, lane < left, g);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Few tokens: one launch.  Every workgroup reads them all; the one of the first place of a token finds the others by comparison, a quarter of
+// the list per wave, and adds up their rows.
+// ---------------------------------------------------------------------------------------------
+
+constexpr int FEW = 1024;
+
+template <int IN, int OUT, int VEC, bool ACC>
+__device__ void sum_few(const Tokens& tokens, const void* dy, long long ld_dy, int own, int col, bool mine, const Grad& g, int32_t* flags)
+{
+    __shared__ Cols<VEC> part[3][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = tokens.n;
+    const int share = (n + 255) / 256 * 64, first = wave * share;            // places of this wave
+    uint32_t keys[FEW / 256];
+#pragma unroll
+    for (int b = 0; b < FEW / 256; ++b) {
+        const int i = first + b * 64 + lane;
+        keys[b] = b * 64 < share && i < n ? key_of_token(tokens, i, (int)g.rows, nullptr) : g.rows;
+    }
+    const uint32_t key = key_of_token(tokens, own, (int)g.rows, flags);
+    if (key == g.rows) return;
+    uint64_t same[FEW / 256];
+    bool seen = false;
+#pragma unroll
+    for (int b = 0; b < FEW / 256; ++b) {
+        same[b] = __ballot(keys[b] == key);
+        if (same[b] && first + b * 64 + __builtin_ctzll(same[b]) < own) seen = true;
+    }
+    if (__syncthreads_or(seen)) return;
+    Cols<VEC> sum = {}, before = {};
+    if (ACC && wave == 0 && mine) before = load_before<OUT, VEC>(g, key, col);
+#pragma unroll
+    for (int b = 0; b < FEW / 256; ++b) {
+        uint64_t left = same[b];
+        while (left) {
+            Cols<VEC> x[AHEAD];
+            int count = 0;
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (left) {
+                    const long long row = first + b * 64 + __builtin_ctzll(left);
+                    left &= left - 1;
+                    if (mine) x[u] = load_cols<IN, VEC>(dy, row * ld_dy + col);
+                    count = u + 1;
+                }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (u < count && mine) add(sum, x[u]);
+        }
+    }
+    if (wave > 0) part[wave - 1][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && mine) {
+#pragma unroll
+        for (int w = 0; w < 3; ++w) add(sum, part[w][lane]);
+        write_sum<OUT, ACC, VEC>(g, key, col, sum, before);
+    }
+}
+
+template <int IN, int OUT, int VEC, bool ACC>
+__global__ __launch_bounds__(256) void grad_of_few(Tokens tokens, const void* dy, long long ld_dy, Grad g, int tiles, unsigned groups, int zero_per, int32_t* flags)
+{
+    const int lane = threadIdx.x & 63;
+    if (blockIdx.x < groups) {
+        for (unsigned w = blockIdx.x; w < (unsigned)tokens.n * (unsigned)tiles; w += groups) {
+            const int own = (int)(w / tiles), tile = (int)(w % tiles);
+            const int first = tile * (64 * VEC), left = g.cols - first;
+            if (left >= VEC) sum_few<IN, OUT, VEC, ACC>(tokens, dy, ld_dy, own, min(first + lane * VEC, g.cols - VEC), lane * VEC < left, g, flags);
+            else sum_few<IN, OUT, 1, ACC>(tokens, dy, ld_dy, own, first + lane, lane < left, g, flags);
+            __syncthreads();
+        }
+        return;
+    }
+    __shared__ uint8_t named[ZERO_ROWS];
+    for (unsigned long long b = blockIdx.x - groups; b * zero_per < g.rows; b += gridDim.x - groups) {
+        const uint32_t first = (uint32_t)(b * zero_per), end = min(first + (uint32_t)zero_per, g.rows);
+        named[threadIdx.x] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < FEW / 256; ++q) {
+            const int i = q * 256 + threadIdx.x;
+            const uint32_t key = i < tokens.n ? key_of_token(tokens, i, (int)g.rows, nullptr) : g.rows;
+            if (key >= first && key < end) named[key - first] = 1;
+        }
+        __syncthreads();
+        write_zeros<OUT>(named, first, end, g);
+        __syncthreads();
     }
 }
 
@@ -471,8 +627,7 @@ struct Layout {
     uint32_t* keys[2];
     uint32_t* from[2];
     int* counts;
-    int* totals;
-    int passes, bits, parts, per;
+    int passes, bits, parts, per;      // passes == 0: by rank
     float* heads;
     float* tails;
     long long ld;                      // of a row of those
@@ -484,9 +639,11 @@ Layout layout_of(void* base, int64_t n, int64_t rows, int cols)
 {
     Layout l = {};
     const int bits = 64 - __builtin_clzll((unsigned long long)rows);             // of keys 0 .. rows
-    l.passes = (bits + 9) / 10;
-    l.bits = (bits + l.passes - 1) / l.passes;
-    l.per = (int)std::max<int64_t>(1024, (n + MOST_PARTS * 256 - 1) / (MOST_PARTS * 256) * 256);
+    l.passes = n <= RANKED ? 0 : (bits + MOST_BITS - 1) / MOST_BITS;
+    l.bits = l.passes ? (bits + l.passes - 1) / l.passes : 0;
+    // 4096 keys per part, four rounds of its waves; more when that would be more parts than a workgroup can add up in passing
+    const int64_t parts = n <= 1 << 20 ? 64 : 256;
+    l.per = (int)std::max<int64_t>(4096, (n + parts * 1024 - 1) / (parts * 1024) * 1024);
     l.parts = (int)((n + l.per - 1) / l.per);
     // long pieces write fewer rows that have to be joined, short ones make more waves: 64 tokens from 4096 waves on
     const int64_t tiles = (cols + 511) / 512;
@@ -500,7 +657,6 @@ Layout layout_of(void* base, int64_t n, int64_t rows, int cols)
         l.from[k] = c.take<uint32_t>(n);
     }
     l.counts = c.take<int>((size_t)l.parts << l.bits);
-    l.totals = c.take<int>((size_t)1 << l.bits);
     l.heads = c.take<float>(l.pieces * l.ld);
     l.tails = c.take<float>(l.pieces * l.ld);
     l.bytes = c.off;
@@ -535,44 +691,56 @@ int embedding_grad(atomo_ctx* ctx, const atomo_tokens& tokens, const atomo_rows&
                    bool accumulate, hipStream_t stream)
 {
     if (tokens.n == 0 && accumulate) return ATOMO_OK;
-    const int rc = workspace_for_stream(ctx, layout_of(nullptr, tokens.n, grad.rows, grad.cols).bytes, stream);
+    const bool few = tokens.n <= FEW;
+    const int rc = few ? ATOMO_OK : workspace_for_stream(ctx, layout_of(nullptr, tokens.n, grad.rows, grad.cols).bytes, stream);
     if (rc != ATOMO_OK) return rc;
-    const Layout l = layout_of(ctx->ws, tokens.n, grad.rows, grad.cols);
+    const Layout l = few ? Layout{} : layout_of(ctx->ws, tokens.n, grad.rows, grad.cols);
     const Tokens t = tokens_of(tokens);
+    const Grad g = {grad.data, (long long)grad.ld, (uint32_t)grad.rows, grad.cols, scale};
+    // workgroups that write zeros: 128 KiB of rows each
+    const int64_t row_bytes = (int64_t)grad.cols * type_bytes(grad.type);
+    const int zero_per = (int)std::min<int64_t>(ZERO_ROWS, std::max<int64_t>(4, (128 << 10) / row_bytes));
+    const unsigned zeros = accumulate ? 0 : (unsigned)std::min<int64_t>(MOST_GROUPS / 2, (grad.rows + zero_per - 1) / zero_per);
     ProfScope ps(ctx, ATOMO_K_EMBEDDING, stream);
     int at = 0;
-    if (tokens.n > 0) {
-        for (int p = 0; p < l.passes; ++p) {
-            const Digit d = {p * l.bits, l.bits};
-            const uint32_t* keys = p ? l.keys[at] : nullptr;
-            sort_count<<<l.parts, 256, 0, stream>>>(t, keys, (int)grad.rows, d, l.per, l.counts, ctx->d_flags);
-            sort_sums<<<1 << l.bits, 64, 0, stream>>>(l.counts, l.parts, l.totals);
-            sort_place<<<l.parts, 256, 0, stream>>>(t, keys, p ? l.from[at] : nullptr, (int)grad.rows, d, l.per, l.counts, l.totals,
-                                                    l.keys[1 - at], l.from[1 - at]);
-            at = 1 - at;
-        }
+    if (!few && l.passes == 0) sort_by_rank<<<(t.n + 63) / 64, 1024, 0, stream>>>(t, (int)grad.rows, l.keys[0], l.from[0], ctx->d_flags);
+    for (int p = 0; p < l.passes; ++p) {
+        const Digit d = {p * l.bits, l.bits};
+        const uint32_t* keys = p ? l.keys[at] : nullptr;
+        sort_count<<<l.parts, 1024, 0, stream>>>(t, keys, (int)grad.rows, d, l.per, l.counts, ctx->d_flags);
+        sort_place<<<l.parts, 1024, 0, stream>>>(t, keys, p ? l.from[at] : nullptr, (int)grad.rows, d, l.per, l.parts, l.counts,
+                                                 l.keys[1 - at], l.from[1 - at]);
+        at = 1 - at;
     }
     const Pieces pieces = {l.keys[at], l.from[at], t.n, l.length, l.heads, l.tails, l.ld};
-    const Grad g = {grad.data, (long long)grad.ld, (uint32_t)grad.rows, grad.cols, scale, accumulate ? 1 : 0};
     with_type(dy.type, [&](auto in) {
         with_type(grad.type, [&](auto ty) {
-            const auto launch = [&](auto vec) {
+            const auto launch = [&](auto vec, auto acc) {
                 const int tiles = (grad.cols - 1) / (64 * vec) + 1;
-                const unsigned groups = (unsigned)std::min<int64_t>(MOST_GROUPS / 2, ((int64_t)l.pieces * tiles + 3) / 4);
-                const int64_t row_bytes = (int64_t)grad.cols * type_bytes(grad.type);
-                const int zero_per = (int)std::min<int64_t>(ZERO_ROWS, std::max<int64_t>(4, (128 << 10) / row_bytes));
-                const unsigned zeros = accumulate ? 0 : (unsigned)std::min<int64_t>(MOST_GROUPS / 2, (grad.rows + zero_per - 1) / zero_per);
-                sum_pieces<in, ty, vec><<<groups + zeros, 256, 0, stream>>>(pieces, dy.data, dy.ld, g, l.pieces, tiles, groups, zero_per);
+                if (few) {
+                    const unsigned groups = (unsigned)std::min<int64_t>(MOST_GROUPS / 2, tokens.n * tiles);
+                    grad_of_few<in, ty, vec, acc><<<groups + zeros, 256, 0, stream>>>(t, dy.data, dy.ld, g, tiles, groups, zero_per, ctx->d_flags);
+                } else {
+                    const unsigned groups = (unsigned)std::min<int64_t>(MOST_GROUPS / 2, ((int64_t)l.pieces * tiles + 3) / 4);
+                    sum_pieces<in, ty, vec, acc><<<groups + zeros, 256, 0, stream>>>(pieces, dy.data, dy.ld, g, l.pieces, tiles, groups, zero_per);
+                }
             };
             // few columns: as many lanes as there are, with less each
             constexpr int WIDE = in == ATOMO_F32 ? 4 : 8, NARROW = in == ATOMO_F32 ? 1 : 2;
-            if (grad.cols <= 64 * NARROW) launch(std::integral_constant<int, NARROW>());
-            else launch(std::integral_constant<int, WIDE>());
+            const auto launch_vec = [&](auto acc) {
+                if (grad.cols <= 64 * NARROW) launch(std::integral_constant<int, NARROW>(), acc);
+                else launch(std::integral_constant<int, WIDE>(), acc);
+            };
+            if (accumulate) launch_vec(std::true_type());
+            else launch_vec(std::false_type());
         });
     });
-    if (l.pieces > 1) {
-        const dim3 grid((unsigned)((l.pieces + 63) / 64), (unsigned)std::min(256, (grad.cols - 1) / 256 + 1));
-        with_type(grad.type, [&](auto ty) { join_pieces<ty><<<grid, 1024, 0, stream>>>(pieces, g, l.pieces); });
+    if (!few) {
+        const dim3 grid((unsigned)((l.pieces + JOINED - 1) / JOINED), (unsigned)std::min(256, (grad.cols - 1) / 256 + 1));
+        with_type(grad.type, [&](auto ty) {
+            if (accumulate) join_pieces<ty, true><<<grid, 1024, 0, stream>>>(pieces, g, l.pieces);
+            else join_pieces<ty, false><<<grid, 1024, 0, stream>>>(pieces, g, l.pieces);
+        });
     }
     ATOMO_HIP(ctx, hipGetLastError());
     return ATOMO_OK;
