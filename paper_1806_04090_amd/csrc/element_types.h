@@ -10,6 +10,7 @@ namespace atomo {
 // (four elements from an address that is a multiple of one element's size: one instruction all the same)
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint16_t u16x8_any __attribute__((ext_vector_type(8), aligned(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 inline int type_bytes(int type) { return type == ATOMO_F32 ? 4 : 2; }

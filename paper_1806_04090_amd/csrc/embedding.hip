@@ -21,16 +21,25 @@ struct Tokens {
     int n, bytes;
 };
 
-__device__ inline long long token_at(const Tokens& t, long long i)
+// The row of a token, or -1 (padding), -2 (outside of the table).
+__device__ inline int row_of(const Tokens& t, long long token, int rows)
 {
-    return t.bytes == 8 ? ((const long long*)t.data)[i] : (long long)((const int*)t.data)[i];
+    return token == t.padding ? -1 : token < 0 || token >= rows ? -2 : (int)token;
 }
 
-// The row of a token, or -1 (padding), -2 (outside of the table).
-__device__ inline int row_of(const Tokens& t, long long i, int rows)
+// Where keys come from: an array of them, or tokens of 4 or 8 bytes (which the loads of a round must not branch on).
+enum { KEYS = 0, TOKENS4 = 4, TOKENS8 = 8 };
+
+template <int SOURCE>
+__device__ inline long long token_at(const Tokens& t, long long i)
 {
-    const long long token = token_at(t, i);
-    return token == t.padding ? -1 : token < 0 || token >= rows ? -2 : (int)token;
+    if constexpr (SOURCE == TOKENS8) return ((const long long*)t.data)[i];
+    else return (long long)((const int*)t.data)[i];
+}
+
+__device__ inline long long token_at(const Tokens& t, long long i)
+{
+    return t.bytes == 8 ? token_at<TOKENS8>(t, i) : token_at<TOKENS4>(t, i);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -43,7 +52,7 @@ __global__ __launch_bounds__(256) void embedding_rows(Tokens tokens, const void*
 {
     const int x = threadIdx.x % lanes_x, y = threadIdx.x / lanes_x, per = 256 / lanes_x;
     for (long long t = (long long)blockIdx.x * per + y; t < tokens.n; t += (long long)gridDim.x * per) {
-        const int row = row_of(tokens, t, rows);
+        const int row = row_of(tokens, token_at(tokens, t), rows);
         if (row == -2 && x == 0) flags[FLAG_TOKEN] = 1;
         for (int col = x * 8; col < cols; col += lanes_x * 8) {
             if (col + 8 <= cols) {
@@ -66,9 +75,9 @@ __global__ __launch_bounds__(256) void embedding_rows(Tokens tokens, const void*
 // ---------------------------------------------------------------------------------------------
 
 // The key of a token: its row, or `rows` if it has none.
-__device__ inline uint32_t key_of_token(const Tokens& t, long long i, int rows, int32_t* flags)
+__device__ inline uint32_t key_of(const Tokens& t, long long token, int rows, int32_t* flags)
 {
-    const int row = row_of(t, i, rows);
+    const int row = row_of(t, token, rows);
     if (row == -2 && flags) flags[FLAG_TOKEN] = 1;
     return row < 0 ? (uint32_t)rows : (uint32_t)row;
 }
@@ -77,13 +86,21 @@ __device__ inline uint32_t key_of_token(const Tokens& t, long long i, int rows, 
 // A workgroup has 64 tokens, one per lane of each of its sixteen waves, which share the keys to compare with.
 constexpr int RANKED = 8192;
 
+template <int SOURCE>
 __global__ __launch_bounds__(1024) void sort_by_rank(Tokens tokens, int rows, uint32_t* keys_out, uint32_t* from_out, int32_t* flags)
 {
     __shared__ uint32_t keys[RANKED];
     __shared__ int ranks[16][64];
     const int n = tokens.n, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int blocks = (n + 63) / 64, own = blockIdx.x;
-    for (int i = threadIdx.x; i < blocks * 64; i += 1024) keys[i] = i < n ? key_of_token(tokens, i, rows, flags) : 0xffffffffu;
+    long long token[RANKED / 1024];
+#pragma unroll
+    for (int k = 0; k < RANKED / 1024; ++k) token[k] = token_at<SOURCE>(tokens, min(k * 1024 + (int)threadIdx.x, n - 1));
+#pragma unroll
+    for (int k = 0; k < RANKED / 1024; ++k) {
+        const int i = k * 1024 + threadIdx.x;
+        if (i < blocks * 64) keys[i] = i < n ? key_of(tokens, token[k], rows, flags) : 0xffffffffu;
+    }
     __syncthreads();
     const uint32_t key = keys[own * 64 + lane];
     int rank = 0;
@@ -115,12 +132,15 @@ constexpr int ROUNDS = 4;              // keys of a lane that are on their way a
 
 struct Digit { int shift, bits; };
 
+template <int SOURCE>
 __device__ inline uint32_t key_at(const Tokens& t, const uint32_t* keys, long long i, int rows, int32_t* flags)
 {
-    return keys ? keys[i] : key_of_token(t, i, rows, flags);
+    if constexpr (SOURCE == KEYS) return keys[i];
+    else return key_of(t, token_at<SOURCE>(t, i), rows, flags);
 }
 
 // counts[part][digit]
+template <int SOURCE>
 __global__ __launch_bounds__(1024) void sort_count(Tokens tokens, const uint32_t* keys, int rows, Digit d, int per, int* counts, int32_t* flags)
 {
     __shared__ int hist[MOST_BINS];
@@ -128,44 +148,69 @@ __global__ __launch_bounds__(1024) void sort_count(Tokens tokens, const uint32_t
     if ((int)threadIdx.x < bins) hist[threadIdx.x] = 0;
     __syncthreads();
     const long long first = (long long)blockIdx.x * per, end = min(first + per, (long long)tokens.n);
-    for (long long i = first + threadIdx.x; i < end; i += 1024) atomicAdd(&hist[key_at(tokens, keys, i, rows, flags) >> d.shift & (bins - 1)], 1);
+    for (long long base = first + threadIdx.x; base < end; base += 1024 * ROUNDS) {
+        uint32_t key[ROUNDS];
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) key[r] = key_at<SOURCE>(tokens, keys, min(base + r * 1024, end - 1), rows, flags);
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r)
+            if (base + r * 1024 < end) atomicAdd(&hist[key[r] >> d.shift & (bins - 1)], 1);
+    }
     __syncthreads();
     if ((int)threadIdx.x < bins) counts[(long long)blockIdx.x * bins + threadIdx.x] = hist[threadIdx.x];
 }
 
 // Each wave takes a sixteenth of the part, 64 keys after the other: a key's place is that of its digit, plus what the waves in front and the
-// keys in front of it have of the same digit.
+// keys in front of it have of the same digit.  Bound by the latency of its loads.
+template <int SOURCE>
 __global__ __launch_bounds__(1024) void sort_place(Tokens tokens, const uint32_t* keys, const uint32_t* from, int rows, Digit d, int per,
                                                    int parts, const int* counts, uint32_t* keys_out, uint32_t* from_out)
 {
     __shared__ int at[16][MOST_BINS];
+    __shared__ int before[MOST_BINS], totals[MOST_BINS];
     __shared__ int sums[8];
     const int bins = 1 << d.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int b = threadIdx.x; b < 16 * MOST_BINS; b += 1024) ((int*)at)[b] = 0;
-    __syncthreads();
     const long long first = (long long)blockIdx.x * per + wave * (per / 16);
     const long long end = min(first + per / 16, (long long)tokens.n);
-    for (long long base = first; base < end; base += 64 * ROUNDS) {
-        uint32_t key[ROUNDS];
+    uint32_t key[ROUNDS], source[ROUNDS];
+    const auto load = [&](long long base, bool sources) {
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
-            const long long i = base + r * 64 + lane;
-            key[r] = i < end ? key_at(tokens, keys, i, rows, nullptr) : 0;
+            const long long i = min(base + r * 64 + lane, (long long)tokens.n - 1);   // (what is beyond the end is not looked at)
+            key[r] = key_at<SOURCE>(tokens, keys, i, rows, nullptr);
+            if (sources) source[r] = SOURCE == KEYS ? from[i] : (uint32_t)i;
         }
+    };
+    // how often each digit comes in the parts in front, and at all: a thread per digit and share of the parts
+    const int digit = (int)threadIdx.x & (bins - 1), stride = 1024 >> d.bits;
+    int in_front = 0, in_all = 0;
+    for (int p = (int)threadIdx.x >> d.bits; p < parts; p += 16 * stride) {
+        int c[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) c[q] = counts[((long long)min(p + q * stride, parts - 1) << d.bits) + digit];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const int part = p + q * stride;
+            in_all += part < parts ? c[q] : 0;
+            in_front += part < (int)blockIdx.x ? c[q] : 0;
+        }
+    }
+    load(first, true);
+    for (int b = threadIdx.x; b < 16 * MOST_BINS; b += 1024) ((int*)at)[b] = 0;
+    if (threadIdx.x < MOST_BINS) before[threadIdx.x] = totals[threadIdx.x] = 0;
+    __syncthreads();
+    if (in_all) {
+        atomicAdd(&totals[digit], in_all);
+        atomicAdd(&before[digit], in_front);
+    }
+    for (long long base = first; base < end; base += 64 * ROUNDS) {
+        if (base > first) load(base, false);
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r)
             if (base + r * 64 + lane < end) atomicAdd(&at[wave][key[r] >> d.shift & (bins - 1)], 1);
     }
-    // a thread per digit: how often it comes in the parts in front, and at all
-    int before = 0, total = 0;
-    if ((int)threadIdx.x < bins) {
-#pragma unroll 16
-        for (int p = 0; p < parts; ++p) {
-            const int c = counts[(long long)p * bins + threadIdx.x];
-            total += c;
-            before += p < (int)blockIdx.x ? c : 0;
-        }
-    }
+    __syncthreads();
+    const int total = (int)threadIdx.x < bins ? totals[threadIdx.x] : 0;
     int sum = total;                                             // of the digits up to this one, first within the wave
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) {
@@ -175,7 +220,7 @@ __global__ __launch_bounds__(1024) void sort_place(Tokens tokens, const uint32_t
     if (wave < 8 && lane == 63) sums[wave] = sum;
     __syncthreads();
     if ((int)threadIdx.x < bins) {
-        int place = before + sum - total;
+        int place = before[threadIdx.x] + sum - total;
         for (int w = 0; w < wave; ++w) place += sums[w];
 #pragma unroll
         for (int w = 0; w < 16; ++w) {
@@ -186,13 +231,7 @@ __global__ __launch_bounds__(1024) void sort_place(Tokens tokens, const uint32_t
     }
     __syncthreads();
     for (long long base = first; base < end; base += 64 * ROUNDS) {
-        uint32_t key[ROUNDS], source[ROUNDS];
-#pragma unroll
-        for (int r = 0; r < ROUNDS; ++r) {
-            const long long i = base + r * 64 + lane;
-            key[r] = i < end ? key_at(tokens, keys, i, rows, nullptr) : 0;
-            source[r] = i < end && from ? from[i] : (uint32_t)i;
-        }
+        if (per > 16 * 64 * ROUNDS) load(base, true);            // (else they are those from the beginning)
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
             const bool live = base + r * 64 + lane < end;
@@ -231,8 +270,7 @@ __device__ inline Cols<VEC> load_cols(const void* base, long long i)
     if constexpr (VEC == 1) {
         c.x[0] = load1<TYPE>(base, i);
     } else if constexpr (VEC == 8 && TYPE != ATOMO_F32) {
-        typedef uint16_t eight __attribute__((ext_vector_type(8), aligned(2)));
-        const eight s = *(const eight*)((const uint16_t*)base + i);
+        const u16x8_any s = *(const u16x8_any*)((const uint16_t*)base + i);
 #pragma unroll
         for (int k = 0; k < 8; ++k) c.x[k] = Element<TYPE>::up(s[k]);
     } else if constexpr (VEC % 4 == 0) {
@@ -259,11 +297,10 @@ __device__ inline void store_cols(void* base, long long i, const Cols<VEC>& c)
     if constexpr (VEC == 1) {
         store1<TYPE>(base, i, c.x[0]);
     } else if constexpr (VEC == 8 && TYPE != ATOMO_F32) {
-        typedef uint16_t eight __attribute__((ext_vector_type(8), aligned(2)));
-        eight s;
+        u16x8_any s;
 #pragma unroll
         for (int k = 0; k < 8; ++k) s[k] = Element<TYPE>::down(c.x[k]);
-        *(eight*)((uint16_t*)base + i) = s;
+        *(u16x8_any*)((uint16_t*)base + i) = s;
     } else if constexpr (VEC % 4 == 0) {
 #pragma unroll
         for (int q = 0; q < VEC / 4; ++q) store4<TYPE>(base, i + 4 * q, f32x4{c.x[4 * q], c.x[4 * q + 1], c.x[4 * q + 2], c.x[4 * q + 3]});
@@ -317,12 +354,16 @@ struct Pieces {
     float* heads;
     float* tails;
     long long ld;
+    uint32_t* notes;                   // of each piece: what its last run does, and the run's key behind it
 };
+
+// The last run of a piece ends in it; begins in it and goes on; fills it, having begun in front of it, and goes on.
+enum : uint32_t { ENDS = 0, BEGINS = 1, PASSES = 2 };
 
 constexpr int AHEAD = 8;               // rows on their way at a time
 
 template <int IN, int OUT, int VEC, bool ACC>
-__device__ void sum_piece(const Pieces& s, int piece, const void* dy, long long ld_dy, int col, bool mine, const Grad& g)
+__device__ void sum_piece(const Pieces& s, int piece, bool noting, const void* dy, long long ld_dy, int col, bool mine, const Grad& g)
 {
     const int lane = threadIdx.x & 63, first = piece * s.length;
     const int here = min(s.length, s.n - first);
@@ -330,11 +371,18 @@ __device__ void sum_piece(const Pieces& s, int piece, const void* dy, long long 
     const uint32_t from = lane < here ? s.from[first + lane] : 0;
     const uint32_t in_front = first > 0 ? s.keys[first - 1] : g.rows, behind = first + s.length < s.n ? s.keys[first + s.length] : g.rows;
     const int count = __popcll(__ballot(key < g.rows));          // (those of no row stand behind all others)
-    if (count == 0) return;
+    if (count == 0) {
+        if (noting && lane == 0) s.notes[2 * piece] = ENDS;
+        return;
+    }
     const bool begun = in_front == (uint32_t)__builtin_amdgcn_readfirstlane((int)key);
     const bool goes_on = count == s.length && behind == (uint32_t)__builtin_amdgcn_readlane((int)key, count - 1);
     const uint32_t next = (uint32_t)__shfl_down((int)key, 1);
     const uint64_t ends = __ballot(lane < count && (lane == count - 1 || key != next));
+    if (noting && lane == 0) {
+        s.notes[2 * piece] = !goes_on ? ENDS : begun && ends == 1ull << (count - 1) ? PASSES : BEGINS;
+        s.notes[2 * piece + 1] = behind;
+    }
     Cols<VEC> sum = {};
     bool in_first = true;
     for (int i = 0; i < count; i += AHEAD) {
@@ -429,7 +477,9 @@ __device__ void zero_rows(const uint32_t* keys, int n, uint32_t first, int per, 
     write_zeros<OUT>(named, first, end, g);
 }
 
-// Waves of the first workgroups take a piece and a tile of columns each; the workgroups behind them write the zeros.
+// Waves of the first workgroups take a piece and a tile of columns each; the workgroups behind them write the zeros.  (On a stream of their
+// own beside the sort, with a byte per row for what the tokens name, the zeros slowed the sort's loads by more than they gained: 170 us
+// for 32,768 tokens into 65,536 x 2048, 174 so.)
 template <int IN, int OUT, int VEC, bool ACC>
 __global__ __launch_bounds__(256) void sum_pieces(Pieces s, const void* dy, long long ld_dy, Grad g, int pieces, int tiles, unsigned groups, int zero_per)
 {
@@ -444,26 +494,28 @@ __global__ __launch_bounds__(256) void sum_pieces(Pieces s, const void* dy, long
     for (long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); w < (long long)pieces * tiles; w += (long long)groups * 4) {
         const int piece = __builtin_amdgcn_readfirstlane((int)(w / tiles)), tile = __builtin_amdgcn_readfirstlane((int)(w % tiles));
         const int first = tile * (64 * VEC), left = g.cols - first;
-        if (left >= VEC) sum_piece<IN, OUT, VEC, ACC>(s, piece, dy, ld_dy, min(first + lane * VEC, g.cols - VEC), lane * VEC < left, g);
-        else sum_piece<IN, OUT, 1, ACC>(s, piece, dy, ld_dy, first + lane, lane < left, g);
+        if (left >= VEC) sum_piece<IN, OUT, VEC, ACC>(s, piece, tile == 0, dy, ld_dy, min(first + lane * VEC, g.cols - VEC), lane * VEC < left, g);
+        else sum_piece<IN, OUT, 1, ACC>(s, piece, tile == 0, dy, ld_dy, first + lane, lane < left, g);
     }
 }
 
 // Runs over several pieces: the tail of the piece in which a run begins, and the heads of those behind it up to its end.  A
-// workgroup looks after JOINED pieces and 256 columns; a wave adds up to SHORT rows by itself, longer runs are shared out among the sixteen.
+// workgroup looks after JOINED pieces and 256 columns; a wave adds up to SHORT rows by itself, longer runs are shared out among the
+// sixteen.  Bound by latency: the notes, then the rows, then the store (found by searching the keys instead, the ends took ten loads one
+// after the other: 16 - 24 us).
 constexpr int SHORT = 16, JOINED = 16;
 
-// The sum of rows [k, end), AHEAD of them on their way at a time.
+// The sum of rows [k, end), sixteen of them on their way at a time.
 template <int VEC>
 __device__ inline void add_rows(Cols<VEC>& sum, const float* rows, long long ld, int k, int end, int col)
 {
-    for (; k < end; k += AHEAD) {
-        Cols<VEC> x[AHEAD];
+    for (; k < end; k += 2 * AHEAD) {
+        Cols<VEC> x[2 * AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
+        for (int u = 0; u < 2 * AHEAD; ++u)
             if (k + u < end) x[u] = load_cols<ATOMO_F32, VEC>(rows, (k + u) * ld + col);
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
+        for (int u = 0; u < 2 * AHEAD; ++u)
             if (k + u < end) add(sum, x[u]);
     }
 }
@@ -473,21 +525,14 @@ __device__ void join_tile(const Pieces& s, int pieces, int base, int col, bool m
 {
     __shared__ Cols<VEC> part[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    // this lane's piece: where the run that begins there ends
+    // lane k: the note of piece base + k; a run that begins in one ends in the first behind it that is not passed
     const int piece = base + lane;
-    int last = 0;
-    uint32_t key = g.rows;
-    const long long end = (long long)(piece + 1) * s.length;
-    if (lane < JOINED && piece < pieces && end < s.n) {
-        key = s.keys[end - 1];
-        const uint32_t first = s.keys[end - s.length], in_front = piece ? s.keys[end - s.length - 1] : g.rows, behind = s.keys[end];
-        if (key < g.rows && (first != key || in_front != key) && behind == key) {
-            last = piece + 1;                                    // the pieces behind whose first key is this one
-#pragma unroll
-            for (int k = 1; k <= SHORT; ++k) last += piece + 1 + k < pieces && s.keys[end + (long long)k * s.length] == key ? 1 : 0;
-        }
-    }
-    const uint64_t runs = __ballot(last > 0), longer = __ballot(last - piece > SHORT && last > 0);
+    const uint32_t note = piece < pieces ? s.notes[2 * piece] : ENDS;
+    const uint32_t key = piece < pieces ? s.notes[2 * piece + 1] : 0;
+    const uint64_t stops = __ballot(note != PASSES);
+    const uint64_t behind = lane < 63 ? stops >> (lane + 1) : 0;
+    const int last = behind ? piece + 1 + __builtin_ctzll(behind) : piece + 64;   // (beyond these 64: further below)
+    const uint64_t runs = __ballot(lane < JOINED && note == BEGINS), longer = __ballot(last - piece > SHORT);
     int turn = 0;
     for (uint64_t left = runs & ~longer; left; left &= left - 1, ++turn) {
         const int at = __builtin_ctzll(left);
@@ -500,10 +545,27 @@ __device__ void join_tile(const Pieces& s, int pieces, int base, int col, bool m
         add_rows(sum, s.heads, s.ld, p + 1, q + 1, col);
         write_sum<OUT, ACC, VEC>(g, row, col, sum, before);
     }
-    for (uint64_t left = longer; left; left &= left - 1) {
+    for (uint64_t left = runs & longer; left; left &= left - 1) {
         const int at = __builtin_ctzll(left);
         const uint32_t row = (uint32_t)__builtin_amdgcn_readlane((int)key, at);
-        const int p = base + at, q = (keys_below(s.keys, s.n, row + 1) - 1) / s.length, share = (q - p + 15) / 16;
+        const int p = base + at;
+        int q = __builtin_amdgcn_readlane(last, at);
+        if (!(stops >> at >> 1)) {                               // 256 notes at a time
+            for (q = base + 64;; q += 256) {
+                uint32_t more[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) more[k] = q + k * 64 + lane < pieces ? s.notes[2 * (q + k * 64 + lane)] : ENDS;
+                uint64_t stop[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) stop[k] = __ballot(more[k] != PASSES);
+                const int k = stop[0] ? 0 : stop[1] ? 1 : stop[2] ? 2 : 3;
+                const uint64_t found = k == 0 ? stop[0] : k == 1 ? stop[1] : k == 2 ? stop[2] : stop[3];
+                if (!found) continue;
+                q += k * 64 + __builtin_ctzll(found);
+                break;
+            }
+        }
+        const int share = (q - p + 15) / 16;
         const int k0 = p + 1 + wave * share, k1 = min(k0 + share, q + 1);
         Cols<VEC> sum = {}, before = {};
         if (mine) add_rows(sum, s.heads, s.ld, k0, k1, col);
@@ -540,6 +602,21 @@ __global__ __launch_bounds__(1024) void join_pieces(Pieces s, Grad g, int pieces
 
 constexpr int FEW = 1024;
 
+// Keys of the tokens first, first + step, ..., all loaded before one is looked at; `rows` from `end` on.
+__device__ inline void keys_of_few(const Tokens& tokens, int first, int step, int end, int rows, uint32_t (&keys)[FEW / 256])
+{
+    long long token[FEW / 256] = {};
+    const auto load = [&](auto source) {
+#pragma unroll
+        for (int b = 0; b < FEW / 256; ++b) token[b] = token_at<source>(tokens, min(first + b * step, tokens.n - 1));
+    };
+    if (tokens.n == 0) end = 0;                                  // (there is none to stand in for those beyond the end)
+    else if (tokens.bytes == 8) load(std::integral_constant<int, TOKENS8>());
+    else load(std::integral_constant<int, TOKENS4>());
+#pragma unroll
+    for (int b = 0; b < FEW / 256; ++b) keys[b] = first + b * step < end ? key_of(tokens, token[b], rows, nullptr) : (uint32_t)rows;
+}
+
 template <int IN, int OUT, int VEC, bool ACC>
 __device__ void sum_few(const Tokens& tokens, const void* dy, long long ld_dy, int own, int col, bool mine, const Grad& g, int32_t* flags)
 {
@@ -547,12 +624,8 @@ __device__ void sum_few(const Tokens& tokens, const void* dy, long long ld_dy, i
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = tokens.n;
     const int share = (n + 255) / 256 * 64, first = wave * share;            // places of this wave
     uint32_t keys[FEW / 256];
-#pragma unroll
-    for (int b = 0; b < FEW / 256; ++b) {
-        const int i = first + b * 64 + lane;
-        keys[b] = b * 64 < share && i < n ? key_of_token(tokens, i, (int)g.rows, nullptr) : g.rows;
-    }
-    const uint32_t key = key_of_token(tokens, own, (int)g.rows, flags);
+    keys_of_few(tokens, first + lane, 64, min(first + share, n), (int)g.rows, keys);
+    const uint32_t key = key_of(tokens, token_at(tokens, own), (int)g.rows, flags);
     if (key == g.rows) return;
     uint64_t same[FEW / 256];
     bool seen = false;
@@ -611,12 +684,11 @@ __global__ __launch_bounds__(256) void grad_of_few(Tokens tokens, const void* dy
         const uint32_t first = (uint32_t)(b * zero_per), end = min(first + (uint32_t)zero_per, g.rows);
         named[threadIdx.x] = 0;
         __syncthreads();
+        uint32_t keys[FEW / 256];
+        keys_of_few(tokens, threadIdx.x, 256, tokens.n, (int)g.rows, keys);
 #pragma unroll
-        for (int q = 0; q < FEW / 256; ++q) {
-            const int i = q * 256 + threadIdx.x;
-            const uint32_t key = i < tokens.n ? key_of_token(tokens, i, (int)g.rows, nullptr) : g.rows;
-            if (key >= first && key < end) named[key - first] = 1;
-        }
+        for (int q = 0; q < FEW / 256; ++q)
+            if (keys[q] >= first && keys[q] < end) named[keys[q] - first] = 1;
         __syncthreads();
         write_zeros<OUT>(named, first, end, g);
         __syncthreads();
@@ -632,6 +704,7 @@ struct Layout {
     float* tails;
     long long ld;                      // of a row of those
     int pieces, length;
+    uint32_t* notes;
     size_t bytes;
 };
 
@@ -641,9 +714,9 @@ Layout layout_of(void* base, int64_t n, int64_t rows, int cols)
     const int bits = 64 - __builtin_clzll((unsigned long long)rows);             // of keys 0 .. rows
     l.passes = n <= RANKED ? 0 : (bits + MOST_BITS - 1) / MOST_BITS;
     l.bits = l.passes ? (bits + l.passes - 1) / l.passes : 0;
-    // 4096 keys per part, four rounds of its waves; more when that would be more parts than a workgroup can add up in passing
+    // as few rounds of a workgroup's waves as 64 parts allow, whose counts it adds up in passing
     const int64_t parts = n <= 1 << 20 ? 64 : 256;
-    l.per = (int)std::max<int64_t>(4096, (n + parts * 1024 - 1) / (parts * 1024) * 1024);
+    l.per = (int)std::max<int64_t>(1024, (n + parts * 1024 - 1) / (parts * 1024) * 1024);
     l.parts = (int)((n + l.per - 1) / l.per);
     // long pieces write fewer rows that have to be joined, short ones make more waves: 64 tokens from 4096 waves on
     const int64_t tiles = (cols + 511) / 512;
@@ -659,6 +732,7 @@ Layout layout_of(void* base, int64_t n, int64_t rows, int cols)
     l.counts = c.take<int>((size_t)l.parts << l.bits);
     l.heads = c.take<float>(l.pieces * l.ld);
     l.tails = c.take<float>(l.pieces * l.ld);
+    l.notes = c.take<uint32_t>(2 * (size_t)l.pieces);
     l.bytes = c.off;
     return l;
 }
@@ -703,16 +777,21 @@ int embedding_grad(atomo_ctx* ctx, const atomo_tokens& tokens, const atomo_rows&
     const unsigned zeros = accumulate ? 0 : (unsigned)std::min<int64_t>(MOST_GROUPS / 2, (grad.rows + zero_per - 1) / zero_per);
     ProfScope ps(ctx, ATOMO_K_EMBEDDING, stream);
     int at = 0;
-    if (!few && l.passes == 0) sort_by_rank<<<(t.n + 63) / 64, 1024, 0, stream>>>(t, (int)grad.rows, l.keys[0], l.from[0], ctx->d_flags);
+    if (!few && l.passes == 0) {
+        const auto kernel = t.bytes == 8 ? sort_by_rank<TOKENS8> : sort_by_rank<TOKENS4>;
+        kernel<<<(t.n + 63) / 64, 1024, 0, stream>>>(t, (int)grad.rows, l.keys[0], l.from[0], ctx->d_flags);
+    }
     for (int p = 0; p < l.passes; ++p) {
         const Digit d = {p * l.bits, l.bits};
         const uint32_t* keys = p ? l.keys[at] : nullptr;
-        sort_count<<<l.parts, 1024, 0, stream>>>(t, keys, (int)grad.rows, d, l.per, l.counts, ctx->d_flags);
-        sort_place<<<l.parts, 1024, 0, stream>>>(t, keys, p ? l.from[at] : nullptr, (int)grad.rows, d, l.per, l.parts, l.counts,
-                                                 l.keys[1 - at], l.from[1 - at]);
+        const auto count = p ? sort_count<KEYS> : t.bytes == 8 ? sort_count<TOKENS8> : sort_count<TOKENS4>;
+        const auto place = p ? sort_place<KEYS> : t.bytes == 8 ? sort_place<TOKENS8> : sort_place<TOKENS4>;
+        count<<<l.parts, 1024, 0, stream>>>(t, keys, (int)grad.rows, d, l.per, l.counts, ctx->d_flags);
+        place<<<l.parts, 1024, 0, stream>>>(t, keys, p ? l.from[at] : nullptr, (int)grad.rows, d, l.per, l.parts, l.counts,
+                                            l.keys[1 - at], l.from[1 - at]);
         at = 1 - at;
     }
-    const Pieces pieces = {l.keys[at], l.from[at], t.n, l.length, l.heads, l.tails, l.ld};
+    const Pieces pieces = {l.keys[at], l.from[at], t.n, l.length, l.heads, l.tails, l.ld, l.notes};
     with_type(dy.type, [&](auto in) {
         with_type(grad.type, [&](auto ty) {
             const auto launch = [&](auto vec, auto acc) {
