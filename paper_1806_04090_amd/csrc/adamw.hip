@@ -16,9 +16,11 @@ namespace atomo {
 
 namespace {
 
-constexpr int CHUNK = 4096;            // elements of a workgroup of 256 threads, four times four per thread
-constexpr int BLOCK8 = 128;            // elements of an 8-bit state with one scale: four of each of 32 lanes
+constexpr int CHUNK = 2048;            // elements of a workgroup of 256 threads, eight per thread
+constexpr int BLOCK8 = 128;            // elements of an 8-bit state with one scale: eight of each of 16 lanes
 constexpr int NORM_PARTS = 2048;       // partial sums of a norm
+
+constexpr bool ONCE_LOADS = true, ONCE_STORES = true;
 
 struct Tensor {
     float* param;
@@ -104,7 +106,7 @@ __device__ inline void adamw_element(const StepArgs& a, const Rates& r, float g,
 
 __device__ inline f32x4 load_any4(int type, const void* base, long long i)
 {
-    return type == ATOMO_F32 ? load4<ATOMO_F32>(base, i) : type == ATOMO_BF16 ? load4<ATOMO_BF16>(base, i) : load4<ATOMO_F16>(base, i);
+    return type == ATOMO_F32 ? load4<ATOMO_F32, ONCE_LOADS>(base, i) : type == ATOMO_BF16 ? load4<ATOMO_BF16, ONCE_LOADS>(base, i) : load4<ATOMO_F16, ONCE_LOADS>(base, i);
 }
 
 __device__ inline float load_any1(int type, const void* base, long long i)
@@ -114,9 +116,9 @@ __device__ inline float load_any1(int type, const void* base, long long i)
 
 __device__ inline void store_any4(int type, void* base, long long i, f32x4 x)
 {
-    if (type == ATOMO_F32) store4<ATOMO_F32>(base, i, x);
-    else if (type == ATOMO_BF16) store4<ATOMO_BF16>(base, i, x);
-    else store4<ATOMO_F16>(base, i, x);
+    if (type == ATOMO_F32) store4<ATOMO_F32, ONCE_STORES>(base, i, x);
+    else if (type == ATOMO_BF16) store4<ATOMO_BF16, ONCE_STORES>(base, i, x);
+    else store4<ATOMO_F16, ONCE_STORES>(base, i, x);
 }
 
 __device__ inline void store_any1(int type, void* base, long long i, float x)
@@ -140,16 +142,16 @@ __global__ __launch_bounds__(256) void adamw_states32(const Tensor* tensors, con
         const long long i = first + k * 1024 + threadIdx.x * 4;
         if (i + 4 <= t.n) {
             const f32x4 g = load_any4(t.grad_type, t.grad, i);
-            f32x4 p4 = load4<ATOMO_F32>(t.param, i), m4 = load4<ATOMO_F32>(m, i), v4 = load4<ATOMO_F32>(v, i);
+            f32x4 p4 = load4<ATOMO_F32, ONCE_LOADS>(t.param, i), m4 = load4<ATOMO_F32, ONCE_LOADS>(m, i), v4 = load4<ATOMO_F32, ONCE_LOADS>(v, i);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float pe = p4[e], me = m4[e], ve = v4[e];
                 adamw_element(a, r, g[e], pe, me, ve);
                 p4[e] = pe; m4[e] = me; v4[e] = ve;
             }
-            store4<ATOMO_F32>(t.param, i, p4);
-            store4<ATOMO_F32>(m, i, m4);
-            store4<ATOMO_F32>(v, i, v4);
+            store4<ATOMO_F32, ONCE_STORES>(t.param, i, p4);
+            store4<ATOMO_F32, ONCE_STORES>(m, i, m4);
+            store4<ATOMO_F32, ONCE_STORES>(v, i, v4);
             if (t.copy) store_any4(t.copy_type, t.copy, i, p4);
         } else {
             for (long long j = i; j < t.n; ++j) {
@@ -210,99 +212,137 @@ __device__ inline uint32_t v_code(float x, int e, uint32_t r)
     return c == 0 && x > 0.0f ? 1u : c;                          // (a v of zero under an m that is not would be a step without bound)
 }
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// The larger of each half of x and of another lane's x.
+template <int FROM>
+__device__ inline uint32_t max_u16x2(uint32_t x)
+{
+    const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, FROM, 0xf, 0xf, false);
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, other)));
+}
+
+// The largest of each half of x over the sixteen lanes of a row: neighbours, pairs, the mirror images of eight lanes and of sixteen.
+__device__ inline uint32_t row_max_u16x2(uint32_t x) { return max_u16x2<0x140>(max_u16x2<0x141>(max_u16x2<0x4e>(max_u16x2<0xb1>(x)))); }
+
+// Eight elements per thread, four in each half of a block: a scale belongs to the sixteen lanes of a row, and what a row loads or
+// stores at a time fills whole cache lines.
 __global__ __launch_bounds__(256) void adamw_states8(const Tensor* tensors, const Chunk* chunks, StepArgs a)
 {
     const Chunk c = chunks[blockIdx.x];
     const Tensor t = tensors[c.tensor];
     Rates r;
     if (!rates_of(a, t, r)) return;
-    const long long first = (long long)c.chunk * CHUNK;
+    const long long first = (long long)c.chunk * CHUNK + threadIdx.x / 16 * BLOCK8, block = first / BLOCK8;
+    const long long at[2] = {first + threadIdx.x % 16 * 4, first + threadIdx.x % 16 * 4 + BLOCK8 / 2};
+    const bool live = first < t.n, whole = first + BLOCK8 <= t.n;            // (the same for the lanes of a row)
     uint8_t* const mc = (uint8_t*)t.m;
     uint8_t* const vc = (uint8_t*)t.v;
-    for (int k = 0; k < CHUNK / 1024; ++k) {
-        const long long i = first + k * 1024 + threadIdx.x * 4;
-        if (first + k * 1024 + (threadIdx.x & ~63) * 4 >= t.n) break;          // (no lane of the wave has an element)
-        const long long block = i / BLOCK8;
-        const int left = (int)(t.n - i < 4 ? (t.n - i > 0 ? t.n - i : 0) : 4);
-        const bool any = left > 0;
-        float p[4] = {0, 0, 0, 0}, m[4], v[4], g[4] = {0, 0, 0, 0};
-        uint32_t mq = 0, vq = 0;
-        const int em = block_exponent(any ? t.m_scale[block] : 0), ev = block_exponent(any ? t.v_scale[block] : 0);
-        if (left == 4) {
-            const f32x4 p4 = load4<ATOMO_F32>(t.param, i), g4 = load_any4(t.grad_type, t.grad, i);
-            __builtin_memcpy(&mq, mc + i, 4);
-            __builtin_memcpy(&vq, vc + i, 4);
+    float p[8], g[8], m[8], v[8];
+    uint32_t mq[2] = {0, 0}, vq[2] = {0, 0};
+    const int m_scale = live ? t.m_scale[block] : 0, v_scale = live ? t.v_scale[block] : 0;
+    if (whole) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { p[e] = p4[e]; g[e] = g4[e]; }
-        } else {
+        for (int h = 0; h < 2; ++h) {
+            __builtin_memcpy(&mq[h], mc + at[h], 4);
+            __builtin_memcpy(&vq[h], vc + at[h], 4);
+            const f32x4 p4 = load4<ATOMO_F32, ONCE_LOADS>(t.param, at[h]), g4 = load_any4(t.grad_type, t.grad, at[h]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < left) {
-                    p[e] = t.param[i + e];
-                    g[e] = load_any1(t.grad_type, t.grad, i + e);
-                    mq |= (uint32_t)mc[i + e] << (8 * e);
-                    vq |= (uint32_t)vc[i + e] << (8 * e);
-                }
+            for (int e = 0; e < 4; ++e) { p[4 * h + e] = p4[e]; g[4 * h + e] = g4[e]; }
         }
-        uint32_t sm = 0, sv = 0;
+    } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            m[e] = m_value(mq >> (8 * e) & 0xff, em);
-            v[e] = v_value(vq >> (8 * e) & 0xff, ev);
-            adamw_element(a, r, g[e], p[e], m[e], v[e]);
-            if (finite(m[e])) sm = max(sm, __float_as_uint(m[e]) >> 23 & 0xff);
-            if (finite(v[e])) sv = max(sv, __float_as_uint(v[e]) >> 23);
+        for (int e = 0; e < 8; ++e) {
+            const long long i = at[e / 4] + e % 4;
+            p[e] = g[e] = 0.0f;
+            if (i < t.n) {
+                p[e] = t.param[i];
+                g[e] = load_any1(t.grad_type, t.grad, i);
+                mq[e / 4] |= (uint32_t)mc[i] << (8 * (e % 4));
+                vq[e / 4] |= (uint32_t)vc[i] << (8 * (e % 4));
+            }
         }
+    }
+    const int em = block_exponent(m_scale), ev = block_exponent(v_scale);
+    uint32_t sm = 0, sv = 0;
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) {
-            sm = max(sm, (uint32_t)__shfl_xor((int)sm, d));
-            sv = max(sv, (uint32_t)__shfl_xor((int)sv, d));
-        }
-        const int fm = block_exponent((int)sm), fv = block_exponent((int)sv);
-        const u32x4 w = philox4x32_10((uint64_t)(t.first_block * (BLOCK8 / 4) + i / 4), (uint64_t)r.step, a.seed);
+    for (int e = 0; e < 8; ++e) {
+        m[e] = m_value(mq[e / 4] >> (8 * (e % 4)) & 0xff, em);
+        v[e] = v_value(vq[e / 4] >> (8 * (e % 4)) & 0xff, ev);
+        adamw_element(a, r, g[e], p[e], m[e], v[e]);
+        if (finite(m[e])) sm = max(sm, __float_as_uint(m[e]) >> 23 & 0xff);
+        if (finite(v[e])) sv = max(sv, __float_as_uint(v[e]) >> 23);
+    }
+    const uint32_t largest = row_max_u16x2(sm << 16 | sv);
+    sm = largest >> 16;
+    sv = largest & 0xffff;
+    const int fm = block_exponent((int)sm), fv = block_exponent((int)sv);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const u32x4 w = philox4x32_10((uint64_t)(t.first_block * (BLOCK8 / 4) + at[h] / 4), (uint64_t)r.step, a.seed);
         const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-        mq = vq = 0;
+        mq[h] = vq[h] = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            mq |= m_code(m[e], fm, words[e] & 0xffff) << (8 * e);
-            vq |= v_code(v[e], fv, words[e] >> 16) << (8 * e);
+            mq[h] |= m_code(m[4 * h + e], fm, words[e] & 0xffff) << (8 * e);
+            vq[h] |= v_code(v[4 * h + e], fv, words[e] >> 16) << (8 * e);
         }
-        if (left == 4) {
-            const f32x4 p4 = {p[0], p[1], p[2], p[3]};
-            store4<ATOMO_F32>(t.param, i, p4);
-            if (t.copy) store_any4(t.copy_type, t.copy, i, p4);
-            __builtin_memcpy(mc + i, &mq, 4);
-            __builtin_memcpy(vc + i, &vq, 4);
-        } else {
+    }
+    if (whole) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < left) {
-                    t.param[i + e] = p[e];
-                    if (t.copy) store_any1(t.copy_type, t.copy, i + e, p[e]);
-                    mc[i + e] = (uint8_t)(mq >> (8 * e));
-                    vc[i + e] = (uint8_t)(vq >> (8 * e));
-                }
+        for (int h = 0; h < 2; ++h) {
+            const f32x4 p4 = {p[4 * h], p[4 * h + 1], p[4 * h + 2], p[4 * h + 3]};
+            store4<ATOMO_F32, ONCE_STORES>(t.param, at[h], p4);
+            if (t.copy) store_any4(t.copy_type, t.copy, at[h], p4);
+            __builtin_memcpy(mc + at[h], &mq[h], 4);
+            __builtin_memcpy(vc + at[h], &vq[h], 4);
         }
-        if (any && (threadIdx.x & 31) == 0) {
-            t.m_scale[block] = (uint8_t)sm;
-            t.v_scale[block] = (uint8_t)sv;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const long long i = at[e / 4] + e % 4;
+            if (i < t.n) {
+                t.param[i] = p[e];
+                if (t.copy) store_any1(t.copy_type, t.copy, i, p[e]);
+                mc[i] = (uint8_t)(mq[e / 4] >> (8 * (e % 4)));
+                vc[i] = (uint8_t)(vq[e / 4] >> (8 * (e % 4)));
+            }
         }
+    }
+    if (live && threadIdx.x % 16 == 0) {
+        t.m_scale[block] = (uint8_t)sm;
+        t.v_scale[block] = (uint8_t)sv;
     }
 }
 
+// Sixteen codes per load: one byte read and two or four written per element.  (Four per load reached 2.8 TB/s.)
 template <int TYPE, bool V>
 __global__ __launch_bounds__(256) void state8_values(const uint8_t* codes, const uint8_t* scales, long long n, void* out)
 {
-    const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+    const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 16;
     if (i >= n) return;
     const int e = block_exponent(scales[i / BLOCK8]);
-    if (i + 4 <= n) {
-        uint32_t q;
-        __builtin_memcpy(&q, codes + i, 4);
-        f32x4 x;
+    if (i + 16 <= n) {
+        uint32_t q[4];
+        __builtin_memcpy(q, codes + i, 16);
+        float x[16];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = V ? v_value(q >> (8 * k) & 0xff, e) : m_value(q >> (8 * k) & 0xff, e);
-        store4<TYPE>(out, i, x);
+        for (int k = 0; k < 16; ++k) {
+            const uint32_t code = q[k / 4] >> (8 * (k % 4)) & 0xff;
+            x[k] = V ? v_value(code, e) : m_value(code, e);
+        }
+        if constexpr (TYPE == ATOMO_F32) {
+#pragma unroll
+            for (int k = 0; k < 16; k += 4) store4<TYPE>(out, i + k, f32x4{x[k], x[k + 1], x[k + 2], x[k + 3]});
+        } else {
+#pragma unroll
+            for (int k = 0; k < 16; k += 8) {
+                u16x8_any s;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[j] = Element<TYPE>::down(x[k + j]);
+                *(u16x8_any*)((uint16_t*)out + i + k) = s;
+            }
+        }
     } else {
         for (long long j = i; j < n; ++j) store1<TYPE>(out, j, V ? v_value(codes[j], e) : m_value(codes[j], e));
     }
@@ -535,7 +575,7 @@ int state8_unpack(atomo_ctx* ctx, int which, const uint8_t* codes, const uint8_t
                   hipStream_t stream)
 {
     ProfScope ps(ctx, ATOMO_K_ADAMW, stream);
-    const unsigned grid = (unsigned)((n + 1023) / 1024);
+    const unsigned grid = (unsigned)((n + 4095) / 4096);
     with_type(type, [&](auto ty) {
         if (which == ATOMO_STATE_V) state8_values<ty, true><<<grid, 256, 0, stream>>>(codes, scales, n, out);
         else state8_values<ty, false><<<grid, 256, 0, stream>>>(codes, scales, n, out);

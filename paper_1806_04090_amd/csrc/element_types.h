@@ -37,20 +37,24 @@ template <> struct Element<ATOMO_F16> {
     __device__ static Stored down(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
 };
 
-template <int TYPE>
+// ONCE: what a kernel reads or writes once and the caches need not keep.
+template <int TYPE, bool ONCE = false>
 __device__ inline f32x4 load4(const void* base, long long i)
 {
-    const auto s = *(const typename Element<TYPE>::Stored4*)((const typename Element<TYPE>::Stored*)base + i);
+    const auto at = (const typename Element<TYPE>::Stored4*)((const typename Element<TYPE>::Stored*)base + i);
+    const auto s = ONCE ? __builtin_nontemporal_load(at) : *at;
     return f32x4{Element<TYPE>::up(s[0]), Element<TYPE>::up(s[1]), Element<TYPE>::up(s[2]), Element<TYPE>::up(s[3])};
 }
 
-template <int TYPE>
+template <int TYPE, bool ONCE = false>
 __device__ inline void store4(void* base, long long i, f32x4 x)
 {
     typename Element<TYPE>::Stored4 s;
 #pragma unroll
     for (int k = 0; k < 4; ++k) s[k] = Element<TYPE>::down(x[k]);
-    *(typename Element<TYPE>::Stored4*)((typename Element<TYPE>::Stored*)base + i) = s;
+    const auto at = (typename Element<TYPE>::Stored4*)((typename Element<TYPE>::Stored*)base + i);
+    if constexpr (ONCE) __builtin_nontemporal_store(s, at);
+    else *at = s;
 }
 
 template <int TYPE>
