@@ -48,20 +48,21 @@ __device__ inline long long token_at(const Tokens& t, long long i)
 
 template <int VEC> struct Cols { float x[VEC]; };
 
-template <int TYPE, int VEC>
+template <int TYPE, int VEC, bool ONCE = false>
 __device__ inline Cols<VEC> load_cols(const void* base, long long i)
 {
     Cols<VEC> c;
     if constexpr (VEC == 1) {
         c.x[0] = load1<TYPE>(base, i);
     } else if constexpr (VEC == 8 && TYPE != ATOMO_F32) {
-        const u16x8_any s = *(const u16x8_any*)((const uint16_t*)base + i);
+        const auto at = (const u16x8_any*)((const uint16_t*)base + i);
+        const u16x8_any s = ONCE ? __builtin_nontemporal_load(at) : *at;
 #pragma unroll
         for (int k = 0; k < 8; ++k) c.x[k] = Element<TYPE>::up(s[k]);
     } else if constexpr (VEC % 4 == 0) {
 #pragma unroll
         for (int q = 0; q < VEC / 4; ++q) {
-            const f32x4 v = load4<TYPE>(base, i + 4 * q);
+            const f32x4 v = load4<TYPE, ONCE>(base, i + 4 * q);
 #pragma unroll
             for (int k = 0; k < 4; ++k) c.x[4 * q + k] = v[k];
         }
@@ -157,51 +158,57 @@ __device__ inline uint32_t key_of(const Tokens& t, long long token, int rows, in
     return row < 0 ? (uint32_t)rows : (uint32_t)row;
 }
 
-// Few tokens: the place of each is the number of those in front of it, by comparison with all.  One launch; n^2 comparisons.
-// A workgroup has 64 tokens, one per lane of each of its sixteen waves, which share the keys to compare with.
-constexpr int RANKED = 8192;
+// Up to RANKED tokens: the place of each is the number of those in front of it, by comparison with all.  One launch; n^2 comparisons.
+// A workgroup has 32 tokens, one per lane of each half of its sixteen waves, and the halves share out the keys to compare with.
+// (8192 tokens: 42 us for all of the gradient, 46 with the sort by digits, which takes over from there.)
+constexpr int RANKED = 8192, RANK_TOKENS = 32;
 
 template <int SOURCE>
 __global__ __launch_bounds__(1024) void sort_by_rank(Tokens tokens, int rows, uint32_t* keys_out, uint32_t* from_out, int32_t* flags)
 {
-    __shared__ uint32_t keys[RANKED];
-    __shared__ int ranks[16][64];
-    const int n = tokens.n, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int blocks = (n + 63) / 64, own = blockIdx.x;
+    __shared__ uint4 keys4[RANKED / 4];
+    __shared__ int ranks[32][RANK_TOKENS];
+    uint32_t* const keys = (uint32_t*)keys4;
+    const int n = tokens.n, lane = threadIdx.x % RANK_TOKENS, part = threadIdx.x / RANK_TOKENS;
+    const int blocks = (n + RANK_TOKENS - 1) / RANK_TOKENS, own = blockIdx.x;
     long long token[RANKED / 1024];
 #pragma unroll
     for (int k = 0; k < RANKED / 1024; ++k) token[k] = token_at<SOURCE>(tokens, min(k * 1024 + (int)threadIdx.x, n - 1));
 #pragma unroll
     for (int k = 0; k < RANKED / 1024; ++k) {
         const int i = k * 1024 + threadIdx.x;
-        if (i < blocks * 64) keys[i] = i < n ? key_of(tokens, token[k], rows, flags) : 0xffffffffu;
+        if (i < blocks * RANK_TOKENS) keys[i] = i < n ? key_of(tokens, token[k], rows, flags) : 0xffffffffu;
     }
     __syncthreads();
-    const uint32_t key = keys[own * 64 + lane];
+    const uint32_t key = keys[own * RANK_TOKENS + lane];
     int rank = 0;
-    for (int b = wave; b < blocks; b += 16) {
-        const uint32_t* const other = keys + b * 64;
+    for (int b = part; b < blocks; b += 32) {
+        const uint4* const other = keys4 + b * (RANK_TOKENS / 4);
         // (key, place) in front of (this key, this place); behind the own block equal keys are not
         const uint32_t limit = b < own ? key + 1 : key;          // (keys are below 2^31)
-#pragma unroll 16
-        for (int j = 0; j < 64; ++j) rank += other[j] < limit ? 1 : 0;
+#pragma unroll
+        for (int j = 0; j < RANK_TOKENS / 4; ++j) {
+            const uint4 o = other[j];
+            rank += (o.x < limit ? 1 : 0) + (o.y < limit ? 1 : 0) + (o.z < limit ? 1 : 0) + (o.w < limit ? 1 : 0);
+        }
         if (b == own) {
-            for (int j = 0; j < 64; ++j) rank += other[j] == key && j < lane ? 1 : 0;
+            for (int j = 0; j < RANK_TOKENS; ++j) rank += keys[b * RANK_TOKENS + j] == key && j < lane ? 1 : 0;
         }
     }
-    ranks[wave][lane] = rank;
+    ranks[part][lane] = rank;
     __syncthreads();
-    if (wave == 0 && own * 64 + lane < n) {
+    if (part == 0 && own * RANK_TOKENS + lane < n) {
         int to = 0;
 #pragma unroll
-        for (int w = 0; w < 16; ++w) to += ranks[w][lane];
+        for (int p = 0; p < 32; ++p) to += ranks[p][lane];
         keys_out[to] = key;
-        from_out[to] = (uint32_t)(own * 64 + lane);
+        from_out[to] = (uint32_t)(own * RANK_TOKENS + lane);
     }
 }
 
 // More: least significant digit first, two launches per digit.  A workgroup of sixteen waves has a part of the keys; few parts, so that each
-// can add up the counts of those in front of it by itself.
+// can add up the counts of those in front of it by itself.  (That it counts the keys of all parts itself, in one launch, is no faster at
+// 8193 tokens, and slower from 16,384 on: 42 and 40 us in all, 55 and 43 at 32,768.)
 constexpr int MOST_BITS = 9, MOST_BINS = 1 << MOST_BITS;
 constexpr int ROUNDS = 4;              // keys of a lane that are on their way at a time
 
@@ -336,6 +343,8 @@ __global__ __launch_bounds__(1024) void sort_place(Tokens tokens, const uint32_t
 
 // Lanes of a wave lie side by side on the columns, VEC each.  The last lane moves back to where it ends with the columns: it then forms
 // what its neighbour forms, and stores the same.  A tile of fewer than VEC columns is taken one column per lane.
+constexpr bool ZERO_ONCE = true, DY_ONCE = true, SUM_ONCE = true;
+
 // The gradient, and what of it a call writes.
 struct Grad {
     void* data;
@@ -361,7 +370,7 @@ __device__ inline void write_sum(const Grad& g, uint32_t row, int col, Cols<VEC>
         add(sum, before);
         lanes_in_order();
     }
-    store_cols<OUT, VEC>(g.data, (long long)row * g.ld + col, sum);
+    store_cols<OUT, VEC, SUM_ONCE && VEC * sizeof(typename Element<OUT>::Stored) <= 16>(g.data, (long long)row * g.ld + col, sum);
 }
 
 // Sums of the runs of equal keys among PIECE sorted tokens, by one wave: runs that lie within the piece are written, the
@@ -412,7 +421,7 @@ __device__ void sum_piece(const Pieces& s, int piece, bool noting, const void* d
                 const long long row = (long long)(uint32_t)__builtin_amdgcn_readlane((int)from, i + u);
                 const uint32_t to = (uint32_t)__builtin_amdgcn_readlane((int)key, i + u);
                 if (mine) {
-                    x[u] = load_cols<IN, VEC>(dy, row * ld_dy + col);
+                    x[u] = load_cols<IN, VEC, DY_ONCE>(dy, row * ld_dy + col);
                     if constexpr (ACC) {
                         if (ends >> (i + u) & 1) before[u] = load_before<OUT, VEC>(g, to, col);
                     }
@@ -462,7 +471,7 @@ __device__ inline void write_zeros(const uint8_t* named, uint32_t first, uint32_
     for (uint32_t r = first + wave; r < end; r += 4) {
         if (named[r - first]) continue;
         for (int col = lane * VEC; col < g.cols; col += 64 * VEC) {
-            if (col + VEC <= g.cols) store_cols<OUT, VEC>(g.data, (long long)r * g.ld + col, zero);
+            if (col + VEC <= g.cols) store_cols<OUT, VEC, ZERO_ONCE>(g.data, (long long)r * g.ld + col, zero);
             else for (int j = col; j < g.cols; ++j) store1<OUT>(g.data, (long long)r * g.ld + j, 0.0f);
         }
     }
@@ -616,10 +625,10 @@ __global__ __launch_bounds__(1024) void join_pieces(Pieces s, Grad g, int pieces
 
 // ---------------------------------------------------------------------------------------------
 // Few tokens: one launch.  Every workgroup reads them all; the one of the first place of a token finds the others by comparison, a quarter of
-// the list per wave, and adds up their rows.
+// the list per wave, and adds up their rows.  Up to FEW_GROUPS workgroups: 1024 tokens x 2048 columns 17 us, by pieces 20; 1024 x 4096 31, 22.
 // ---------------------------------------------------------------------------------------------
 
-constexpr int FEW = 1024;
+constexpr int FEW = 2048, FEW_GROUPS = 4096;
 
 // Keys of the tokens first, first + step, ..., all loaded before one is looked at; `rows` from `end` on.
 __device__ inline void keys_of_few(const Tokens& tokens, int first, int step, int end, int rows, uint32_t (&keys)[FEW / 256])
@@ -787,7 +796,8 @@ int embedding_grad(atomo_ctx* ctx, const atomo_tokens& tokens, const atomo_rows&
                    bool accumulate, hipStream_t stream)
 {
     if (tokens.n == 0 && accumulate) return ATOMO_OK;
-    const bool few = tokens.n <= FEW;
+    const int64_t few_tiles = (grad.cols + 511) / 512;
+    const bool few = tokens.n <= FEW && tokens.n * few_tiles <= FEW_GROUPS;
     const int rc = few ? ATOMO_OK : workspace_for_stream(ctx, layout_of(nullptr, tokens.n, grad.rows, grad.cols).bytes, stream);
     if (rc != ATOMO_OK) return rc;
     const Layout l = few ? Layout{} : layout_of(ctx->ws, tokens.n, grad.rows, grad.cols);
@@ -801,7 +811,7 @@ int embedding_grad(atomo_ctx* ctx, const atomo_tokens& tokens, const atomo_rows&
     int at = 0;
     if (!few && l.passes == 0) {
         const auto kernel = t.bytes == 8 ? sort_by_rank<TOKENS8> : sort_by_rank<TOKENS4>;
-        kernel<<<(t.n + 63) / 64, 1024, 0, stream>>>(t, (int)grad.rows, l.keys[0], l.from[0], ctx->d_flags);
+        kernel<<<(t.n + RANK_TOKENS - 1) / RANK_TOKENS, 1024, 0, stream>>>(t, (int)grad.rows, l.keys[0], l.from[0], ctx->d_flags);
     }
     for (int p = 0; p < l.passes; ++p) {
         const Digit d = {p * l.bits, l.bits};
