@@ -92,16 +92,36 @@ __device__ inline bool rates_of(const StepArgs& a, const Tensor& t, Rates& r)
     return true;
 }
 
-// One element.  The products and sums of m and v are rounded each by itself, without fused multiply-adds: the 8-bit codes
+// m and v of one element.  Their products and sums are rounded each by itself, without fused multiply-adds: the 8-bit codes
 // depend on the last bit, and this way they are the same as those of any program that forms the two sums in fp32.
-__device__ inline void adamw_element(const StepArgs& a, const Rates& r, float g, float& p, float& m, float& v)
+__device__ inline void average(const StepArgs& a, const Rates& r, float g, float& m, float& v)
 {
 #pragma clang fp contract(off)
     g = g * r.gs;
     m = a.b1 * m + a.c1 * g;
     v = a.b2 * v + a.c2 * (g * g);
-    const float step = r.rate * (m / (sqrtf(v) * r.root + a.eps));
-    p = p - (step + r.decay * p);
+}
+
+// What `v` has to be for the instruction's square root, which takes numbers below the smallest normal one for zero.
+constexpr uint32_t SMALLEST_ROOT = 0x00800000u;
+
+// The parameters of N elements.  Root and reciprocal are those of the hardware, off by at most one unit in the last place each (the
+// update by 13 half units in all; the exact forms are some twenty instructions per element more).
+template <int N>
+__device__ inline void update(const StepArgs& a, const Rates& r, float (&p)[N], const float (&m)[N], const float (&v)[N])
+{
+    uint32_t least = ~0u;                                        // of the v that are not zero, less one
+#pragma unroll
+    for (int e = 0; e < N; ++e) least = min(least, __float_as_uint(v[e]) - 1);
+    const auto all = [&](auto root) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float step = r.rate * (m[e] * __builtin_amdgcn_rcpf(root(v[e]) * r.root + a.eps));
+            p[e] = p[e] - (step + r.decay * p[e]);
+        }
+    };
+    if (__any(least < SMALLEST_ROOT - 1)) all([](float x) { return sqrtf(x); });
+    else all([](float x) { return __builtin_amdgcn_sqrtf(x); });
 }
 
 __device__ inline f32x4 load_any4(int type, const void* base, long long i)
@@ -142,25 +162,28 @@ __global__ __launch_bounds__(256) void adamw_states32(const Tensor* tensors, con
         const long long i = first + k * 1024 + threadIdx.x * 4;
         if (i + 4 <= t.n) {
             const f32x4 g = load_any4(t.grad_type, t.grad, i);
-            f32x4 p4 = load4<ATOMO_F32, ONCE_LOADS>(t.param, i), m4 = load4<ATOMO_F32, ONCE_LOADS>(m, i), v4 = load4<ATOMO_F32, ONCE_LOADS>(v, i);
+            const f32x4 p4 = load4<ATOMO_F32, ONCE_LOADS>(t.param, i), m4 = load4<ATOMO_F32, ONCE_LOADS>(m, i), v4 = load4<ATOMO_F32, ONCE_LOADS>(v, i);
+            float pe[4], me[4], ve[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float pe = p4[e], me = m4[e], ve = v4[e];
-                adamw_element(a, r, g[e], pe, me, ve);
-                p4[e] = pe; m4[e] = me; v4[e] = ve;
+                pe[e] = p4[e]; me[e] = m4[e]; ve[e] = v4[e];
+                average(a, r, g[e], me[e], ve[e]);
             }
-            store4<ATOMO_F32, ONCE_STORES>(t.param, i, p4);
-            store4<ATOMO_F32, ONCE_STORES>(m, i, m4);
-            store4<ATOMO_F32, ONCE_STORES>(v, i, v4);
-            if (t.copy) store_any4(t.copy_type, t.copy, i, p4);
+            update(a, r, pe, me, ve);
+            const f32x4 new_p = {pe[0], pe[1], pe[2], pe[3]};
+            store4<ATOMO_F32, ONCE_STORES>(t.param, i, new_p);
+            store4<ATOMO_F32, ONCE_STORES>(m, i, f32x4{me[0], me[1], me[2], me[3]});
+            store4<ATOMO_F32, ONCE_STORES>(v, i, f32x4{ve[0], ve[1], ve[2], ve[3]});
+            if (t.copy) store_any4(t.copy_type, t.copy, i, new_p);
         } else {
             for (long long j = i; j < t.n; ++j) {
-                float pe = t.param[j], me = m[j], ve = v[j];
-                adamw_element(a, r, load_any1(t.grad_type, t.grad, j), pe, me, ve);
-                t.param[j] = pe;
-                m[j] = me;
-                v[j] = ve;
-                if (t.copy) store_any1(t.copy_type, t.copy, j, pe);
+                float pe[1] = {t.param[j]}, me[1] = {m[j]}, ve[1] = {v[j]};
+                average(a, r, load_any1(t.grad_type, t.grad, j), me[0], ve[0]);
+                update(a, r, pe, me, ve);
+                t.param[j] = pe[0];
+                m[j] = me[0];
+                v[j] = ve[0];
+                if (t.copy) store_any1(t.copy_type, t.copy, j, pe[0]);
             }
         }
     }
@@ -184,11 +207,27 @@ __device__ inline float m_value(uint32_t code, int e)
     return code & 0x80 ? -y : y;
 }
 
+template <bool NAN_CODES = true>
 __device__ inline float v_value(uint32_t code, int e)
 {
     const float x = ldexpf(__uint_as_float(code << 20), TO_FP32 - V_BIAS + e - V_BIAS);
-    return code == 0xff ? __uint_as_float(0x7fc00000u) : x;
+    return NAN_CODES && code == 0xff ? __uint_as_float(0x7fc00000u) : x;
 }
+
+// Whether one of four codes is 0xff.
+__device__ inline bool has_ff(uint32_t q) { return ((~q - 0x01010101u) & q & 0x80808080u) != 0; }
+
+// Four codes of m at a time: the instruction's format is that of the codes.
+__device__ inline void m_values(uint32_t q, int e, float* m)
+{
+    const float unit = ldexpf(1.0f, e - M_BIAS);
+    m[0] = __builtin_amdgcn_cvt_f32_fp8((int)q, 0) * unit;
+    m[1] = __builtin_amdgcn_cvt_f32_fp8((int)q, 1) * unit;
+    m[2] = __builtin_amdgcn_cvt_f32_fp8((int)q, 2) * unit;
+    m[3] = __builtin_amdgcn_cvt_f32_fp8((int)q, 3) * unit;
+}
+
+__device__ inline bool finite(float x) { return (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u; }
 
 // |x| scaled to where its code's exponent is fp32's; then adding r below the three mantissa bits carries into them with the
 // probability of what is cut off.  (Below the smallest normal code the scaled number is a denormal, rounded to 2^-20 of a step.)
@@ -197,19 +236,30 @@ __device__ inline uint32_t code_of(float x, int exponent, uint32_t r)
     return (__float_as_uint(ldexpf(fabsf(x), exponent)) + (r << 4)) >> 20;
 }
 
-__device__ inline bool finite(float x) { return (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u; }
-
-__device__ inline uint32_t m_code(float x, int e, uint32_t r)
+// Codes of four elements.  FINITE: all of them are.
+template <bool FINITE>
+__device__ inline uint32_t m_codes(const float* x, int e, const uint32_t* words)
 {
-    const uint32_t c = finite(x) ? code_of(x, M_BIAS - e - (TO_FP32 - M_BIAS), r) : 0x7fu;
-    return c | (x < 0.0f ? 0x80u : 0u);
+    uint32_t q = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t c = FINITE || finite(x[k]) ? code_of(x[k], M_BIAS - e - (TO_FP32 - M_BIAS), words[k] & 0xffff) : 0x7fu;
+        q |= (c | (x[k] < 0.0f ? 0x80u : 0u)) << (8 * k);
+    }
+    return q;
 }
 
-__device__ inline uint32_t v_code(float x, int e, uint32_t r)
+template <bool FINITE>
+__device__ inline uint32_t v_codes(const float* x, int e, const uint32_t* words)
 {
-    if (!finite(x)) return 0xffu;
-    const uint32_t c = code_of(x, V_BIAS - e - (TO_FP32 - V_BIAS), r);
-    return c == 0 && x > 0.0f ? 1u : c;                          // (a v of zero under an m that is not would be a step without bound)
+    uint32_t q = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t c = code_of(x[k], V_BIAS - e - (TO_FP32 - V_BIAS), words[k] >> 16);
+        // (a v of zero under an m that is not would be a step without bound)
+        q |= (FINITE || finite(x[k]) ? max(c, min(__float_as_uint(x[k]), 1u)) : 0xffu) << (8 * k);
+    }
+    return q;
 }
 
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
@@ -265,13 +315,29 @@ __global__ __launch_bounds__(256) void adamw_states8(const Tensor* tensors, cons
     }
     const int em = block_exponent(m_scale), ev = block_exponent(v_scale);
     uint32_t sm = 0, sv = 0;
+    m_values(mq[0], em, m);
+    m_values(mq[1], em, m + 4);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = v_value<false>(vq[e / 4] >> (8 * (e % 4)) & 0xff, ev);
+    if (__any(has_ff(vq[0]) || has_ff(vq[1]))) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = v_value(vq[e / 4] >> (8 * (e % 4)) & 0xff, ev);
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        m[e] = m_value(mq[e / 4] >> (8 * (e % 4)) & 0xff, em);
-        v[e] = v_value(vq[e / 4] >> (8 * (e % 4)) & 0xff, ev);
-        adamw_element(a, r, g[e], p[e], m[e], v[e]);
-        if (finite(m[e])) sm = max(sm, __float_as_uint(m[e]) >> 23 & 0xff);
-        if (finite(v[e])) sv = max(sv, __float_as_uint(v[e]) >> 23);
+        average(a, r, g[e], m[e], v[e]);
+        sm = max(sm, __float_as_uint(m[e]) >> 23 & 0xff);
+        sv = max(sv, __float_as_uint(v[e]) >> 23 & 0xff);
+    }
+    update(a, r, p, m, v);
+    const bool finite_all = !__any(sm == 0xff || sv == 0xff);
+    if (!finite_all) {                                           // scales are those of the finite ones
+        sm = sv = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (finite(m[e])) sm = max(sm, __float_as_uint(m[e]) >> 23 & 0xff);
+            if (finite(v[e])) sv = max(sv, __float_as_uint(v[e]) >> 23);
+        }
     }
     const uint32_t largest = row_max_u16x2(sm << 16 | sv);
     sm = largest >> 16;
@@ -281,11 +347,12 @@ __global__ __launch_bounds__(256) void adamw_states8(const Tensor* tensors, cons
     for (int h = 0; h < 2; ++h) {
         const u32x4 w = philox4x32_10((uint64_t)(t.first_block * (BLOCK8 / 4) + at[h] / 4), (uint64_t)r.step, a.seed);
         const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-        mq[h] = vq[h] = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            mq[h] |= m_code(m[4 * h + e], fm, words[e] & 0xffff) << (8 * e);
-            vq[h] |= v_code(v[4 * h + e], fv, words[e] >> 16) << (8 * e);
+        if (finite_all) {
+            mq[h] = m_codes<true>(m + 4 * h, fm, words);
+            vq[h] = v_codes<true>(v + 4 * h, fv, words);
+        } else {
+            mq[h] = m_codes<false>(m + 4 * h, fm, words);
+            vq[h] = v_codes<false>(v + 4 * h, fv, words);
         }
     }
     if (whole) {
