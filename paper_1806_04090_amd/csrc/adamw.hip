@@ -382,36 +382,50 @@ __global__ __launch_bounds__(256) void adamw_states8(const Tensor* tensors, cons
     }
 }
 
-// Sixteen codes per load: one byte read and two or four written per element.  (Four per load reached 2.8 TB/s.)
+// One byte read and two or four written per element, sixteen bytes per store (eight codes of a thread, four where they become fp32), which
+// the caches need not keep, and GROUPS of them on their way at a time.
+constexpr int GROUPS = 2;
+
 template <int TYPE, bool V>
 __global__ __launch_bounds__(256) void state8_values(const uint8_t* codes, const uint8_t* scales, long long n, void* out)
 {
-    const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 16;
-    if (i >= n) return;
-    const int e = block_exponent(scales[i / BLOCK8]);
-    if (i + 16 <= n) {
-        uint32_t q[4];
-        __builtin_memcpy(q, codes + i, 16);
-        float x[16];
+    constexpr int VEC = TYPE == ATOMO_F32 ? 4 : 8;
+    const long long first = ((long long)blockIdx.x * (256 * GROUPS) + threadIdx.x) * VEC;
+    if (((long long)blockIdx.x + 1) * (256 * GROUPS * VEC) <= n) {
+        uint32_t q[GROUPS][VEC / 4];
+        int e[GROUPS];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const uint32_t code = q[k / 4] >> (8 * (k % 4)) & 0xff;
-            x[k] = V ? v_value(code, e) : m_value(code, e);
+        for (int u = 0; u < GROUPS; ++u) {
+            __builtin_memcpy(q[u], codes + first + u * (256 * VEC), VEC);
+            e[u] = scales[(first + u * (256 * VEC)) / BLOCK8];
         }
-        if constexpr (TYPE == ATOMO_F32) {
 #pragma unroll
-            for (int k = 0; k < 16; k += 4) store4<TYPE>(out, i + k, f32x4{x[k], x[k + 1], x[k + 2], x[k + 3]});
-        } else {
+        for (int u = 0; u < GROUPS; ++u) {
+            const long long i = first + u * (256 * VEC);
+            float x[VEC];
 #pragma unroll
-            for (int k = 0; k < 16; k += 8) {
+            for (int h = 0; h < VEC / 4; ++h) {
+                if constexpr (V) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[4 * h + k] = v_value(q[u][h] >> (8 * k) & 0xff, block_exponent(e[u]));
+                } else {
+                    m_values(q[u][h], block_exponent(e[u]), x + 4 * h);
+                }
+            }
+            if constexpr (TYPE == ATOMO_F32) {
+                store4<TYPE, true>(out, i, f32x4{x[0], x[1], x[2], x[3]});
+            } else {
                 u16x8_any s;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s[j] = Element<TYPE>::down(x[k + j]);
-                *(u16x8_any*)((uint16_t*)out + i + k) = s;
+                for (int j = 0; j < 8; ++j) s[j] = Element<TYPE>::down(x[j % VEC]);
+                __builtin_nontemporal_store(s, (u16x8_any*)((uint16_t*)out + i));
             }
         }
     } else {
-        for (long long j = i; j < n; ++j) store1<TYPE>(out, j, V ? v_value(codes[j], e) : m_value(codes[j], e));
+        for (long long i = (long long)blockIdx.x * (256 * GROUPS * VEC) + threadIdx.x; i < n; i += 256) {
+            const int e = block_exponent(scales[i / BLOCK8]);
+            store1<TYPE>(out, i, V ? v_value(codes[i], e) : m_value(codes[i], e));
+        }
     }
 }
 
@@ -642,8 +656,9 @@ int state8_unpack(atomo_ctx* ctx, int which, const uint8_t* codes, const uint8_t
                   hipStream_t stream)
 {
     ProfScope ps(ctx, ATOMO_K_ADAMW, stream);
-    const unsigned grid = (unsigned)((n + 4095) / 4096);
     with_type(type, [&](auto ty) {
+        constexpr int PER = 256 * GROUPS * (ty == ATOMO_F32 ? 4 : 8);
+        const unsigned grid = (unsigned)((n + PER - 1) / PER);
         if (which == ATOMO_STATE_V) state8_values<ty, true><<<grid, 256, 0, stream>>>(codes, scales, n, out);
         else state8_values<ty, false><<<grid, 256, 0, stream>>>(codes, scales, n, out);
     });
