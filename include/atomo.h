@@ -342,7 +342,7 @@ enum { ATOMO_F32 = 0, ATOMO_BF16 = 1, ATOMO_F16 = 2 };
  * row the same; the stride of a single row is not looked at). */
 typedef struct atomo_rows {
     int64_t rows;                    /* < 2^31 - 1; 0 rows only where stated                          */
-    int32_t cols, type;
+    int32_t cols, type;              /* 1 <= cols <= 2^30                                             */
     int64_t ld;
     void* data;                      /* device                                                        */
 } atomo_rows;
@@ -424,7 +424,8 @@ typedef struct atomo_adamw atomo_adamw;   /* opaque: the tensors of a model, des
 
 /* Describes the tensors (HOST array of n, read during the call) on the context's device; waits for the device.  Memory that a step
  * writes may overlap nothing else in the plan: ATOMO_EINVAL, as for tensors of more than 6.8e10 elements together.  Contents stay the caller's: nothing of them is kept.
- * One plan must not be used from two streams at once.  Destroy it before its context. */
+ * One plan must not be used from two streams at once.  Destroy it before its context, and after the graphs that hold its
+ * calls. */
 int atomo_adamw_create(atomo_ctx* ctx, const atomo_adamw_tensor* tensors /*host*/, int n, atomo_adamw** out);
 int atomo_adamw_destroy(atomo_ctx* ctx, atomo_adamw* plan);
 

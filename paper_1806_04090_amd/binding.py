@@ -321,6 +321,7 @@ class Context:
         if not torch.cuda.is_available():
             raise RuntimeError("libatomo needs a GPU: no HIP device is visible and there is no CPU fallback")
         self.device = torch.device("cuda", device)
+        self.index = device
         self._h = C.c_void_p()
         _check(lib().atomo_create(C.byref(self._h), device), "atomo_create")
 
@@ -571,7 +572,7 @@ assert struct.calcsize("ddddqQQQffQ") == C.sizeof(atomo_adamw_options)
 def _stream_of(ctx: Context, stream: Optional[torch.cuda.Stream]) -> int:
     """The stream given, or the current one of the context's device (which need not be the current device)."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(ctx.device.index)
+        return torch._C._cuda_getCurrentRawStream(ctx.index)
     if stream.device != ctx.device:
         raise ValueError(f"the stream is one of {stream.device}, the context of {ctx.device}")
     return int(stream.cuda_stream)
@@ -581,7 +582,7 @@ def _on_device(ctx: Context, t: torch.Tensor, what: str, types) -> int:
     """Checks the type and the device of a tensor; returns its address."""
     if not isinstance(t, torch.Tensor) or t.dtype not in types:
         raise TypeError(f"{what} must be a tensor of {' or '.join(str(x).replace('torch.', '') for x in types)}")
-    if t.device != ctx.device:
+    if t.get_device() != ctx.index:
         raise ValueError(f"{what} is on {t.device}, the context on {ctx.device}")
     return t.data_ptr()
 
@@ -601,15 +602,16 @@ def _pack_rows(ctx: Context, t: torch.Tensor, what: str) -> bytes:
     shape, stride = t.shape, t.stride()
     if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError(f"{what} must be a 2-D tensor with unit column stride")
-    return _PACK_ROWS(shape[0], shape[1], _TYPES[t.dtype], stride[0] if shape[0] > 1 else shape[1], at)
+    rows, cols = shape
+    return _PACK_ROWS(rows, cols, _TYPES[t.dtype], stride[0] if rows > 1 else cols, at)
 
 
-_TOKEN_TYPES = (torch.int64, torch.int32)
+_TOKEN_TYPES = {torch.int64: 8, torch.int32: 4}
 
 
 def _pack_tokens(ctx: Context, tokens: torch.Tensor, padding: int) -> bytes:
     at = _flat(ctx, tokens, "tokens", _TOKEN_TYPES)
-    return _PACK_TOKENS(tokens.numel(), at, tokens.element_size(), padding)
+    return _PACK_TOKENS(tokens.numel(), at, _TOKEN_TYPES[tokens.dtype], padding)
 
 
 def _as_rows(t: torch.Tensor, tokens: torch.Tensor, what: str) -> torch.Tensor:
@@ -768,11 +770,12 @@ def atomo_state8_unpack(ctx: Context, which: str, codes: torch.Tensor, scales: t
     """What the codes of an 8-bit state stand for; which: "m" or "v".  out: float32 (the default) or 16 bits."""
     if which not in ("m", "v"):
         raise ValueError('which is "m" or "v"')
-    n = codes.numel()
+    u8 = (torch.uint8,)
+    codes_at, n = _flat(ctx, codes, "codes", u8), codes.numel()
+    scales_at = _flat(ctx, scales, "scales", u8, -(-n // STATE8_BLOCK))
     if out is None:
         out = torch.empty(n, dtype=torch.float32, device=codes.device)
-    u8 = (torch.uint8,)
-    _check(lib().atomo_state8_unpack(ctx._h, ATOMO_STATE_M if which == "m" else ATOMO_STATE_V, _flat(ctx, codes, "codes", u8),
-                                     _flat(ctx, scales, "scales", u8, -(-n // STATE8_BLOCK)), n, _TYPES[out.dtype] if isinstance(out, torch.Tensor) and out.dtype in _TYPES else -1,
-                                     _flat(ctx, out, "out", _TYPES, n), _stream_of(ctx, stream)), "atomo_state8_unpack")
+    out_at = _flat(ctx, out, "out", _TYPES, n)
+    _check(lib().atomo_state8_unpack(ctx._h, ATOMO_STATE_M if which == "m" else ATOMO_STATE_V, codes_at, scales_at, n, _TYPES[out.dtype],
+                                     out_at, _stream_of(ctx, stream)), "atomo_state8_unpack")
     return out

@@ -517,7 +517,7 @@ namespace {
 
 bool bad_rows(const atomo_rows& m, bool written, bool may_be_empty)
 {
-    if (m.rows < (may_be_empty ? 0 : 1) || m.rows >= INT32_MAX || m.cols < 1 || !known_type(m.type)) return true;
+    if (m.rows < (may_be_empty ? 0 : 1) || m.rows >= INT32_MAX || m.cols < 1 || m.cols > (1 << 30) || !known_type(m.type)) return true;
     if (m.rows > 0 && !m.data) return true;
     return m.rows > 1 && (written || m.ld != 0) && m.ld < m.cols;
 }
@@ -555,7 +555,7 @@ int atomo_embedding_grad(atomo_ctx* ctx, const atomo_tokens* tokens, const atomo
 
 int atomo_embedding_workspace_bytes(int64_t n_tokens, int64_t rows, int32_t cols, size_t* bytes)
 {
-    if (n_tokens < 0 || n_tokens > INT32_MAX || rows < 1 || rows >= INT32_MAX || cols < 1 || !bytes) return ATOMO_EINVAL;
+    if (n_tokens < 0 || n_tokens > INT32_MAX || rows < 1 || rows >= INT32_MAX || cols < 1 || cols > (1 << 30) || !bytes) return ATOMO_EINVAL;
     *bytes = embedding_workspace_bytes(n_tokens, rows, cols);
     return ATOMO_OK;
 }

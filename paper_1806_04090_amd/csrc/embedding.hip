@@ -397,7 +397,7 @@ __device__ void sum_piece(const Pieces& s, int piece, bool noting, const void* d
     const int here = min(s.length, s.n - first);
     const uint32_t key = lane < here ? s.keys[first + lane] : g.rows;
     const uint32_t from = lane < here ? s.from[first + lane] : 0;
-    const uint32_t in_front = first > 0 ? s.keys[first - 1] : g.rows, behind = first + s.length < s.n ? s.keys[first + s.length] : g.rows;
+    const uint32_t in_front = first > 0 ? s.keys[first - 1] : g.rows, behind = s.n - first > s.length ? s.keys[first + s.length] : g.rows;
     const int count = __popcll(__ballot(key < g.rows));          // (those of no row stand behind all others)
     if (count == 0) {
         if (noting && lane == 0) s.notes[2 * piece] = ENDS;
@@ -495,7 +495,7 @@ __device__ void zero_rows(const uint32_t* keys, int n, uint32_t first, int per, 
         const uint32_t row = first + threadIdx.x;
         int lo = bounds[0], up = hi;
         while (lo < up) {
-            const int mid = (lo + up) / 2;
+            const int mid = lo + (up - lo) / 2;
             if (keys[mid] < row) lo = mid + 1;
             else up = mid;
         }

@@ -51,7 +51,7 @@ def grad(toks=None, dy=None, g=None, ctx=DUMMY):
     (lambda: grad(None, rows(5, data=address(2), ld=0)), True),
     (lambda: grad(tokens(0, None), rows(0, data=None)), True),
     (lambda: lookup(ctx=None), False), (lambda: grad(ctx=None), False),
-    (lambda: lookup(rows(0)), False), (lambda: lookup(rows(2 ** 31 - 1)), False), (lambda: lookup(rows(cols=0, ld=1)), False),
+    (lambda: lookup(rows(0)), False), (lambda: lookup(rows(2 ** 31 - 1)), False), (lambda: lookup(rows(cols=0, ld=1)), False), (lambda: lookup(rows(cols=2 ** 30 + 1, ld=2 ** 31), None, rows(5, 2 ** 30 + 1, ATOMO_F32, 2 ** 31, address(2))), False),
     (lambda: lookup(rows(type=3)), False), (lambda: lookup(rows(type=-1)), False), (lambda: lookup(rows(data=None)), False),
     (lambda: lookup(rows(ld=7)), False), (lambda: lookup(rows(ld=-8)), False),
     (lambda: lookup(None, tokens(-1)), False), (lambda: lookup(None, tokens(2 ** 31)), False), (lambda: lookup(None, tokens(data=None)), False),
@@ -149,7 +149,7 @@ def test_workspace_query():
         assert L.atomo_embedding_workspace_bytes(n, r, 64, C.byref(size)) == 0
         assert size.value >= 8 * n
     assert binding.embedding_workspace_bytes(4096, 1000, 64) > 0
-    for n, r, c in ((-1, 1, 1), (2 ** 31, 1, 1), (1, 0, 1), (1, 2 ** 31 - 1, 1), (1, 1, 0)):
+    for n, r, c in ((-1, 1, 1), (2 ** 31, 1, 1), (1, 0, 1), (1, 2 ** 31 - 1, 1), (1, 1, 0), (1, 1, 2 ** 30 + 1)):
         assert L.atomo_embedding_workspace_bytes(n, r, c, C.byref(size)) == ATOMO_EINVAL
     assert L.atomo_embedding_workspace_bytes(1, 1, 1, None) == ATOMO_EINVAL
 
