@@ -1,9 +1,12 @@
 // AdamW over many tensors, the norm of their gradients, and what 8-bit states stand for.
 //
-// Every element is read and written once and has about fourteen operations (twice that, and a third of a Philox block, with 8-bit
+// Every element is read and written once and has about fourteen operations (some fifty, and a quarter of a Philox block, with 8-bit
 // states): the bound is HBM, 28 bytes per element with 32-bit states and gradients, 16 with states in 8 bits.
 // The tensors of a plan are described once on the device; a step is one launch over chunks of CHUNK elements of all of
 // them (two, if both kinds of states occur).
+// Parameters, gradients and states go past the caches, both ways (0.27 billion parameters with bf16 gradients and copies, 28 bytes each:
+// 1.42 ms, 5.3 TB/s, through them; 1.28 ms, 5.9 TB/s, so; loads alone or stores alone gain nothing).  That takes whole cache lines
+// per row of lanes: with eight neighbouring elements per lane and half a line per store, 8-bit states went from 0.85 ms to 1.2.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -16,11 +19,14 @@ namespace atomo {
 
 namespace {
 
-constexpr int CHUNK = 2048;            // elements of a workgroup of 256 threads, eight per thread
+// Elements of a workgroup of 256 threads, eight per thread.  (The 62 tensors of ResNet-18, most of them short, 57 us with a norm and 8-bit
+// states; 62 with 4096, 64 with 8192.)
+constexpr int CHUNK = 2048;
 constexpr int BLOCK8 = 128;            // elements of an 8-bit state with one scale: eight of each of 16 lanes
+// Up to so many chunks a norm is one launch, of a workgroup per chunk: a ticket takes 25 ns, the second launch 2.3 us (one chunk 6.4 -> 4.1
+// us, 64 chunks 6.4 -> 5.4, 128 6.3 -> 7.2).
+constexpr int FEW_CHUNKS = 64;
 constexpr int NORM_PARTS = 2048;       // partial sums of a norm
-
-constexpr bool ONCE_LOADS = true, ONCE_STORES = true;
 
 struct Tensor {
     float* param;
@@ -126,7 +132,7 @@ __device__ inline void update(const StepArgs& a, const Rates& r, float (&p)[N], 
 
 __device__ inline f32x4 load_any4(int type, const void* base, long long i)
 {
-    return type == ATOMO_F32 ? load4<ATOMO_F32, ONCE_LOADS>(base, i) : type == ATOMO_BF16 ? load4<ATOMO_BF16, ONCE_LOADS>(base, i) : load4<ATOMO_F16, ONCE_LOADS>(base, i);
+    return type == ATOMO_F32 ? load4<ATOMO_F32, true>(base, i) : type == ATOMO_BF16 ? load4<ATOMO_BF16, true>(base, i) : load4<ATOMO_F16, true>(base, i);
 }
 
 __device__ inline float load_any1(int type, const void* base, long long i)
@@ -136,9 +142,9 @@ __device__ inline float load_any1(int type, const void* base, long long i)
 
 __device__ inline void store_any4(int type, void* base, long long i, f32x4 x)
 {
-    if (type == ATOMO_F32) store4<ATOMO_F32, ONCE_STORES>(base, i, x);
-    else if (type == ATOMO_BF16) store4<ATOMO_BF16, ONCE_STORES>(base, i, x);
-    else store4<ATOMO_F16, ONCE_STORES>(base, i, x);
+    if (type == ATOMO_F32) store4<ATOMO_F32, true>(base, i, x);
+    else if (type == ATOMO_BF16) store4<ATOMO_BF16, true>(base, i, x);
+    else store4<ATOMO_F16, true>(base, i, x);
 }
 
 __device__ inline void store_any1(int type, void* base, long long i, float x)
@@ -162,7 +168,7 @@ __global__ __launch_bounds__(256) void adamw_states32(const Tensor* tensors, con
         const long long i = first + k * 1024 + threadIdx.x * 4;
         if (i + 4 <= t.n) {
             const f32x4 g = load_any4(t.grad_type, t.grad, i);
-            const f32x4 p4 = load4<ATOMO_F32, ONCE_LOADS>(t.param, i), m4 = load4<ATOMO_F32, ONCE_LOADS>(m, i), v4 = load4<ATOMO_F32, ONCE_LOADS>(v, i);
+            const f32x4 p4 = load4<ATOMO_F32, true>(t.param, i), m4 = load4<ATOMO_F32, true>(m, i), v4 = load4<ATOMO_F32, true>(v, i);
             float pe[4], me[4], ve[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -171,9 +177,9 @@ __global__ __launch_bounds__(256) void adamw_states32(const Tensor* tensors, con
             }
             update(a, r, pe, me, ve);
             const f32x4 new_p = {pe[0], pe[1], pe[2], pe[3]};
-            store4<ATOMO_F32, ONCE_STORES>(t.param, i, new_p);
-            store4<ATOMO_F32, ONCE_STORES>(m, i, f32x4{me[0], me[1], me[2], me[3]});
-            store4<ATOMO_F32, ONCE_STORES>(v, i, f32x4{ve[0], ve[1], ve[2], ve[3]});
+            store4<ATOMO_F32, true>(t.param, i, new_p);
+            store4<ATOMO_F32, true>(m, i, f32x4{me[0], me[1], me[2], me[3]});
+            store4<ATOMO_F32, true>(v, i, f32x4{ve[0], ve[1], ve[2], ve[3]});
             if (t.copy) store_any4(t.copy_type, t.copy, i, new_p);
         } else {
             for (long long j = i; j < t.n; ++j) {
@@ -296,7 +302,7 @@ __global__ __launch_bounds__(256) void adamw_states8(const Tensor* tensors, cons
         for (int h = 0; h < 2; ++h) {
             __builtin_memcpy(&mq[h], mc + at[h], 4);
             __builtin_memcpy(&vq[h], vc + at[h], 4);
-            const f32x4 p4 = load4<ATOMO_F32, ONCE_LOADS>(t.param, at[h]), g4 = load_any4(t.grad_type, t.grad, at[h]);
+            const f32x4 p4 = load4<ATOMO_F32, true>(t.param, at[h]), g4 = load_any4(t.grad_type, t.grad, at[h]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) { p[4 * h + e] = p4[e]; g[4 * h + e] = g4[e]; }
         }
@@ -359,7 +365,7 @@ __global__ __launch_bounds__(256) void adamw_states8(const Tensor* tensors, cons
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const f32x4 p4 = {p[4 * h], p[4 * h + 1], p[4 * h + 2], p[4 * h + 3]};
-            store4<ATOMO_F32, ONCE_STORES>(t.param, at[h], p4);
+            store4<ATOMO_F32, true>(t.param, at[h], p4);
             if (t.copy) store_any4(t.copy_type, t.copy, at[h], p4);
             __builtin_memcpy(mc + at[h], &mq[h], 4);
             __builtin_memcpy(vc + at[h], &vq[h], 4);
@@ -436,6 +442,7 @@ __global__ __launch_bounds__(256) void state8_values(const uint8_t* codes, const
 __device__ double workgroup_sum(double x)
 {
     __shared__ double part[4];
+    __syncthreads();                                             // (it may still be read from a sum before)
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
@@ -478,7 +485,9 @@ __device__ inline double chunk_squares(const void* grad, long long first, long l
     return sum;
 }
 
-__global__ __launch_bounds__(256) void norm_parts(const Tensor* tensors, const Chunk* chunks, int n_chunks, double* parts)
+// LAST: the last of few workgroups to end (by a ticket that it puts back) forms the total in the same launch.
+template <bool LAST>
+__global__ __launch_bounds__(256) void norm_parts(const Tensor* tensors, const Chunk* chunks, int n_chunks, double* parts, unsigned* ticket, float scale, float* norm)
 {
     double sum = 0.0;
     Chunk c = chunks[blockIdx.x];
@@ -493,7 +502,22 @@ __global__ __launch_bounds__(256) void norm_parts(const Tensor* tensors, const C
         c = next;
     }
     sum = workgroup_sum(sum);
-    if (threadIdx.x == 0) parts[blockIdx.x] = sum;
+    if constexpr (LAST) {
+        __shared__ bool last;
+        if (threadIdx.x == 0) {
+            parts[blockIdx.x] = sum;
+            __threadfence();
+            last = atomicInc(ticket, gridDim.x - 1) == gridDim.x - 1;           // (back at zero with the last)
+            __threadfence();
+        }
+        __syncthreads();
+        if (!last) return;
+        const double part = __hip_atomic_load(&parts[min((int)threadIdx.x, (int)gridDim.x - 1)], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        sum = workgroup_sum(threadIdx.x < gridDim.x ? part : 0.0);
+        if (threadIdx.x == 0) norm[0] = (float)((double)scale * sqrt(sum));
+    } else if (threadIdx.x == 0) {
+        parts[blockIdx.x] = sum;
+    }
 }
 
 __global__ __launch_bounds__(256) void norm_total(const double* parts, int n, float scale, float* norm)
@@ -518,6 +542,7 @@ struct atomo_adamw {
     atomo::Tensor* tensors = nullptr;
     atomo::Chunk* chunks = nullptr;    // those of tensors with 32-bit states first
     double* parts = nullptr;
+    unsigned* ticket = nullptr;        // zero between calls
     int n32 = 0, n8 = 0;               // chunks
     bool updates = false;              // has parameters
 };
@@ -584,6 +609,7 @@ int adamw_create(atomo_ctx* ctx, const atomo_adamw_tensor* tensors, int n, atomo
         plan->tensors = c.take<Tensor>(n);
         plan->chunks = c.take<Chunk>(chunks.size());
         plan->parts = c.take<double>(NORM_PARTS);
+        plan->ticket = c.take<unsigned>(1);
         return c.off;
     };
     if (hipMalloc(&plan->dev, carve(nullptr)) != hipSuccess) {
@@ -593,6 +619,7 @@ int adamw_create(atomo_ctx* ctx, const atomo_adamw_tensor* tensors, int n, atomo
     carve(plan->dev);
     hipError_t e = hipMemcpy(plan->tensors, table.data(), n * sizeof(Tensor), hipMemcpyHostToDevice);
     if (e == hipSuccess) e = hipMemcpy(plan->chunks, chunks.data(), chunks.size() * sizeof(Chunk), hipMemcpyHostToDevice);
+    if (e == hipSuccess) e = hipMemset(plan->ticket, 0, sizeof(unsigned));
     if (e == hipSuccess) e = hipDeviceSynchronize();
     if (e != hipSuccess) {
         ctx->last_hip = (int)e;
@@ -618,9 +645,14 @@ bool adamw_updates(const atomo_adamw* plan) { return plan->updates; }
 int adamw_grad_norm(atomo_ctx* ctx, const atomo_adamw* plan, float grad_scale, float* norm, hipStream_t stream)
 {
     ProfScope ps(ctx, ATOMO_K_ADAMW, stream);
-    const int n = plan->n32 + plan->n8, grid = std::min(n, NORM_PARTS);
-    norm_parts<<<grid, 256, 0, stream>>>(plan->tensors, plan->chunks, n, plan->parts);
-    norm_total<<<1, 256, 0, stream>>>(plan->parts, grid, fabsf(grad_scale), norm);
+    const int n = plan->n32 + plan->n8;
+    if (n <= FEW_CHUNKS) {
+        norm_parts<true><<<n, 256, 0, stream>>>(plan->tensors, plan->chunks, n, plan->parts, plan->ticket, fabsf(grad_scale), norm);
+    } else {
+        const int grid = std::min(n, NORM_PARTS);
+        norm_parts<false><<<grid, 256, 0, stream>>>(plan->tensors, plan->chunks, n, plan->parts, nullptr, 0.0f, nullptr);
+        norm_total<<<1, 256, 0, stream>>>(plan->parts, grid, fabsf(grad_scale), norm);
+    }
     ATOMO_HIP(ctx, hipGetLastError());
     return ATOMO_OK;
 }

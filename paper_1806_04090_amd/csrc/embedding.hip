@@ -3,7 +3,7 @@
 // The lookup is a copy of rows: bound by the write of the output and the read of the rows named.
 // The gradient is the sum of the row atoms e_token dy^T.  The tokens are sorted (stably, so that equal ones keep their
 // order), and each row of the table sums the run of its tokens: no atomics on values, one write per row.  Bound by the read of dy
-// and the write of the gradient.
+// and the write of the gradient; from few tokens, by the latency of the launches.
 #include <algorithm>
 #include <cstring>
 
@@ -343,9 +343,8 @@ __global__ __launch_bounds__(1024) void sort_place(Tokens tokens, const uint32_t
 
 // Lanes of a wave lie side by side on the columns, VEC each.  The last lane moves back to where it ends with the columns: it then forms
 // what its neighbour forms, and stores the same.  A tile of fewer than VEC columns is taken one column per lane.
-constexpr bool ZERO_ONCE = true, DY_ONCE = true, SUM_ONCE = true;
+// What is read once (dy) and what is written once (zeros, sums) goes past the caches: 32,768 tokens into 65,536 x 2048 175 -> 162 us.
 
-// The gradient, and what of it a call writes.
 struct Grad {
     void* data;
     long long ld;
@@ -370,10 +369,10 @@ __device__ inline void write_sum(const Grad& g, uint32_t row, int col, Cols<VEC>
         add(sum, before);
         lanes_in_order();
     }
-    store_cols<OUT, VEC, SUM_ONCE && VEC * sizeof(typename Element<OUT>::Stored) <= 16>(g.data, (long long)row * g.ld + col, sum);
+    store_cols<OUT, VEC, VEC * sizeof(typename Element<OUT>::Stored) <= 16>(g.data, (long long)row * g.ld + col, sum);
 }
 
-// Sums of the runs of equal keys among PIECE sorted tokens, by one wave: runs that lie within the piece are written, the
+// Sums of the runs of equal keys among `length` sorted tokens, by one wave: runs that lie within the piece are written, the
 // others go into `heads` (the run has begun in front of the piece) and `tails` (it begins here and does not end), one row per piece each.
 struct Pieces {
     const uint32_t* keys;
@@ -421,7 +420,7 @@ __device__ void sum_piece(const Pieces& s, int piece, bool noting, const void* d
                 const long long row = (long long)(uint32_t)__builtin_amdgcn_readlane((int)from, i + u);
                 const uint32_t to = (uint32_t)__builtin_amdgcn_readlane((int)key, i + u);
                 if (mine) {
-                    x[u] = load_cols<IN, VEC, DY_ONCE>(dy, row * ld_dy + col);
+                    x[u] = load_cols<IN, VEC, true>(dy, row * ld_dy + col);
                     if constexpr (ACC) {
                         if (ends >> (i + u) & 1) before[u] = load_before<OUT, VEC>(g, to, col);
                     }
@@ -471,7 +470,7 @@ __device__ inline void write_zeros(const uint8_t* named, uint32_t first, uint32_
     for (uint32_t r = first + wave; r < end; r += 4) {
         if (named[r - first]) continue;
         for (int col = lane * VEC; col < g.cols; col += 64 * VEC) {
-            if (col + VEC <= g.cols) store_cols<OUT, VEC, ZERO_ONCE>(g.data, (long long)r * g.ld + col, zero);
+            if (col + VEC <= g.cols) store_cols<OUT, VEC, true>(g.data, (long long)r * g.ld + col, zero);
             else for (int j = col; j < g.cols; ++j) store1<OUT>(g.data, (long long)r * g.ld + j, 0.0f);
         }
     }
@@ -796,7 +795,7 @@ int embedding_grad(atomo_ctx* ctx, const atomo_tokens& tokens, const atomo_rows&
                    bool accumulate, hipStream_t stream)
 {
     if (tokens.n == 0 && accumulate) return ATOMO_OK;
-    const int64_t few_tiles = (grad.cols + 511) / 512;
+    const int64_t few_tiles = (grad.cols - 1) / (dy.type == ATOMO_F32 ? 256 : 512) + 1;
     const bool few = tokens.n <= FEW && tokens.n * few_tiles <= FEW_GROUPS;
     const int rc = few ? ATOMO_OK : workspace_for_stream(ctx, layout_of(nullptr, tokens.n, grad.rows, grad.cols).bytes, stream);
     if (rc != ATOMO_OK) return rc;

@@ -93,7 +93,7 @@ SIZES = [[1], [3], [4], [5, 1, 2], [127, 128, 129, 255, 256, 257], [4095, 4096, 
 
 @pytest.mark.parametrize("sizes", SIZES, ids=lambda s: f"{len(s)}x{max(s)}")
 @pytest.mark.parametrize("bits", [32, 8])
-@pytest.mark.parametrize("grad, copy, odd", [(F32, None, False), (BF16, BF16, False), (F16, F16, True), (F32, BF16, True)])
+@pytest.mark.parametrize("grad, copy, odd", [(F32, None, False), (BF16, BF16, False), (F16, F16, True), (F32, BF16, True), (BF16, F32, False)])
 def test_steps(sizes, bits, grad, copy, odd):
     model = Model(sizes, bits, grad, copy, odd, seed=len(sizes))
     for t in (1, 2, 1000):
@@ -301,6 +301,18 @@ def test_a_norm_that_is_not_finite_skips_the_step(bits, wrong):
     model.g[1][12_345] = 0.0
     binding.atomo_adamw_step(ctx(), model.plan, 1e-2, step=2, grad_norm=binding.atomo_adamw_grad_norm(ctx(), model.plan))
     assert not any(torch.equal(a, b) for a, b in zip(model.p[:2], before[:2]))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_the_first_step_is_the_rate_whatever_the_size_of_the_gradient(bits):
+    # from empty states, m / (1 - b1) = g and v / (1 - b2) = g^2: with eps = 0 the step is lr times the sign, down to a v that is an fp32 denormal
+    g = torch.logspace(-19, 17, 5000, device="cuda") * torch.tensor([1.0, -1.0], device="cuda").repeat(2500)
+    p, s = torch.zeros(5000, device="cuda"), binding.alloc_adamw_state(5000, bits, "cuda")
+    binding.atomo_adamw_step(ctx(), binding.AdamwPlan(ctx(), [p], [g], [s]), 1e-2, B1, B2, 0.0, step=1)
+    v = 1e-3 * g.double().square()
+    off = (p.double() + 1e-2 * g.double().sign()).abs() / 1e-2
+    # 13 u and the 5 u of m (here one product), and half of what the three roundings of v lose below the smallest normal number
+    assert (off <= (13 + 5) * U * 1.01 + 0.5 * 3 * 2.0 ** -150 / v).all()
 
 
 def test_zero_gradients_and_zero_eps():
