@@ -635,10 +635,10 @@ __device__ inline void keys_of_few(const Tokens& tokens, int first, int step, in
     long long token[FEW / 256] = {};
     const auto load = [&](auto source) {
 #pragma unroll
-        for (int b = 0; b < FEW / 256; ++b) token[b] = token_at<source>(tokens, min(first + b * step, tokens.n - 1));
+        for (int b = 0; b < FEW / 256; ++b)
+            if (b * 256 < tokens.n) token[b] = token_at<source>(tokens, min(first + b * step, tokens.n - 1));
     };
-    if (tokens.n == 0) end = 0;                                  // (there is none to stand in for those beyond the end)
-    else if (tokens.bytes == 8) load(std::integral_constant<int, TOKENS8>());
+    if (tokens.bytes == 8) load(std::integral_constant<int, TOKENS8>());
     else load(std::integral_constant<int, TOKENS4>());
 #pragma unroll
     for (int b = 0; b < FEW / 256; ++b) keys[b] = first + b * step < end ? key_of(tokens, token[b], rows, nullptr) : (uint32_t)rows;
@@ -658,7 +658,7 @@ __device__ void sum_few(const Tokens& tokens, const void* dy, long long ld_dy, i
     bool seen = false;
 #pragma unroll
     for (int b = 0; b < FEW / 256; ++b) {
-        same[b] = __ballot(keys[b] == key);
+        same[b] = b * 256 < n ? __ballot(keys[b] == key) : 0;
         if (same[b] && first + b * 64 + __builtin_ctzll(same[b]) < own) seen = true;
     }
     if (__syncthreads_or(seen)) return;
