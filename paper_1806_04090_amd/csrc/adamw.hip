@@ -612,14 +612,19 @@ int adamw_create(atomo_ctx* ctx, const atomo_adamw_tensor* tensors, int n, atomo
         plan->ticket = c.take<unsigned>(1);
         return c.off;
     };
-    if (hipMalloc(&plan->dev, carve(nullptr)) != hipSuccess) {
-        (void)hipGetLastError();
-        return ATOMO_ENOMEM;
+    // tables, and a ticket of zero, in one copy
+    std::vector<char> image(carve(nullptr), 0);
+    carve(image.data());
+    memcpy(plan->tensors, table.data(), n * sizeof(Tensor));
+    memcpy(plan->chunks, chunks.data(), chunks.size() * sizeof(Chunk));
+    hipError_t e = hipMalloc(&plan->dev, image.size());
+    if (e != hipSuccess) {
+        (void)hipGetLastError();              // (reported by the status alone: a later call is not to find it)
+        ctx->last_hip = (int)e;
+        return e == hipErrorOutOfMemory ? ATOMO_ENOMEM : ATOMO_EHIP;
     }
     carve(plan->dev);
-    hipError_t e = hipMemcpy(plan->tensors, table.data(), n * sizeof(Tensor), hipMemcpyHostToDevice);
-    if (e == hipSuccess) e = hipMemcpy(plan->chunks, chunks.data(), chunks.size() * sizeof(Chunk), hipMemcpyHostToDevice);
-    if (e == hipSuccess) e = hipMemset(plan->ticket, 0, sizeof(unsigned));
+    e = hipMemcpy(plan->dev, image.data(), image.size(), hipMemcpyHostToDevice);
     if (e == hipSuccess) e = hipDeviceSynchronize();
     if (e != hipSuccess) {
         ctx->last_hip = (int)e;

@@ -764,6 +764,16 @@ Layout layout_of(void* base, int64_t n, int64_t rows, int cols)
     return l;
 }
 
+// Calls f with where keys come from.  (Kernels are launched by name: for a call through a pointer the host sanitizer reads what lies in
+// front of the kernel's handle, and the optimizer then drops the launch as undefined.)
+template <typename F>
+void with_source(const Tokens& t, bool sorted, F&& f)
+{
+    if (sorted) f(std::integral_constant<int, KEYS>());
+    else if (t.bytes == 8) f(std::integral_constant<int, TOKENS8>());
+    else f(std::integral_constant<int, TOKENS4>());
+}
+
 Tokens tokens_of(const atomo_tokens& t) { return Tokens{t.data, (long long)t.padding, (int)t.n, t.bytes}; }
 
 }  // namespace
@@ -782,9 +792,12 @@ int embedding(atomo_ctx* ctx, const atomo_rows& table, const atomo_tokens& token
     ProfScope ps(ctx, ATOMO_K_EMBEDDING, stream);
     with_type(table.type, [&](auto in) {
         with_type(out.type, [&](auto ty) {
-            const auto kernel = many ? embedding_rows<in, ty, TWO_ROWS> : embedding_rows<in, ty, 1>;
-            kernel<<<grid, 256, 0, stream>>>(tokens_of(tokens), table.data, table.ld, (int)table.rows, table.cols, scale,
-                                             out.data, out.ld, lanes_x, ctx->d_flags);
+            const auto launch = [&](auto rows) {
+                embedding_rows<in, ty, rows><<<grid, 256, 0, stream>>>(tokens_of(tokens), table.data, table.ld, (int)table.rows, table.cols,
+                                                                      scale, out.data, out.ld, lanes_x, ctx->d_flags);
+            };
+            if (many) launch(std::integral_constant<int, TWO_ROWS>());
+            else launch(std::integral_constant<int, 1>());
         });
     });
     ATOMO_HIP(ctx, hipGetLastError());
@@ -809,17 +822,17 @@ int embedding_grad(atomo_ctx* ctx, const atomo_tokens& tokens, const atomo_rows&
     ProfScope ps(ctx, ATOMO_K_EMBEDDING, stream);
     int at = 0;
     if (!few && l.passes == 0) {
-        const auto kernel = t.bytes == 8 ? sort_by_rank<TOKENS8> : sort_by_rank<TOKENS4>;
-        kernel<<<(t.n + RANK_TOKENS - 1) / RANK_TOKENS, 1024, 0, stream>>>(t, (int)grad.rows, l.keys[0], l.from[0], ctx->d_flags);
+        with_source(t, false, [&](auto source) {
+            sort_by_rank<source><<<(t.n + RANK_TOKENS - 1) / RANK_TOKENS, 1024, 0, stream>>>(t, (int)grad.rows, l.keys[0], l.from[0], ctx->d_flags);
+        });
     }
     for (int p = 0; p < l.passes; ++p) {
         const Digit d = {p * l.bits, l.bits};
-        const uint32_t* keys = p ? l.keys[at] : nullptr;
-        const auto count = p ? sort_count<KEYS> : t.bytes == 8 ? sort_count<TOKENS8> : sort_count<TOKENS4>;
-        const auto place = p ? sort_place<KEYS> : t.bytes == 8 ? sort_place<TOKENS8> : sort_place<TOKENS4>;
-        count<<<l.parts, 1024, 0, stream>>>(t, keys, (int)grad.rows, d, l.per, l.counts, ctx->d_flags);
-        place<<<l.parts, 1024, 0, stream>>>(t, keys, p ? l.from[at] : nullptr, (int)grad.rows, d, l.per, l.parts, l.counts,
-                                            l.keys[1 - at], l.from[1 - at]);
+        with_source(t, p > 0, [&](auto source) {
+            sort_count<source><<<l.parts, 1024, 0, stream>>>(t, l.keys[at], (int)grad.rows, d, l.per, l.counts, ctx->d_flags);
+            sort_place<source><<<l.parts, 1024, 0, stream>>>(t, l.keys[at], l.from[at], (int)grad.rows, d, l.per, l.parts, l.counts,
+                                                             l.keys[1 - at], l.from[1 - at]);
+        });
         at = 1 - at;
     }
     const Pieces pieces = {l.keys[at], l.from[at], t.n, l.length, l.heads, l.tails, l.ld, l.notes};

@@ -172,3 +172,19 @@ def test_struct_layouts_match_the_header(tmp_path):
         body = re.search(r"typedef struct %s \{(.*?)\} %s;" % (st.__name__, st.__name__), text, flags=re.S).group(1)
         declared = [part.replace("*", " ").split()[-1] for stmt in body.split(";") if stmt.strip() for part in stmt.split(",")]
         assert declared == [name for name, _ in st._fields_], st.__name__
+
+
+def test_kernels_are_launched_by_name():
+    # called through a pointer, a kernel's launch was dropped by the optimizer in the build with the host sanitizer, whose check of such
+    # calls reads in front of the kernel's handle: the second digit of the sort was missing, and what followed read rows from memory never written
+    for name in ("embedding.hip", "adamw.hip"):
+        text = re.sub(r"//.*", "", open(os.path.join(ROOT, "paper_1806_04090_amd", "csrc", name)).read())
+        kernels = set(re.findall(r"__global__[^;{]*?\bvoid\s+(\w+)\s*\(", text))
+        launched = []
+        for m in re.finditer("<<<", text):
+            head, depth = text[:m.start()].rstrip(), 0
+            while head.endswith(">") or depth:                   # template arguments
+                depth += (head[-1] == ">") - (head[-1] == "<")
+                head = head[:-1].rstrip()
+            launched.append(re.search(r"(\w+)$", head)[1])
+        assert launched and set(launched) <= kernels, set(launched) - kernels
