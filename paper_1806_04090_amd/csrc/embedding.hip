@@ -815,9 +815,10 @@ int embedding_grad(atomo_ctx* ctx, const atomo_tokens& tokens, const atomo_rows&
     const Layout l = few ? Layout{} : layout_of(ctx->ws, tokens.n, grad.rows, grad.cols);
     const Tokens t = tokens_of(tokens);
     const Grad g = {grad.data, (long long)grad.ld, (uint32_t)grad.rows, grad.cols, scale};
-    // workgroups that write zeros: 128 KiB of rows each
+    // workgroups that write zeros: at least four rows each, at most 128 KiB, and a thousand workgroups where there are as many rows
+    // (849 rows of 192 columns, bf16, in four workgroups of 256 rows: 14.0 us, now 7.1)
     const int64_t row_bytes = (int64_t)grad.cols * type_bytes(grad.type);
-    const int zero_per = (int)std::min<int64_t>(ZERO_ROWS, std::max<int64_t>(4, (128 << 10) / row_bytes));
+    const int zero_per = (int)std::max<int64_t>(4, std::min<int64_t>(ZERO_ROWS, std::min<int64_t>((128 << 10) / row_bytes, grad.rows / 1024)));
     const unsigned zeros = accumulate ? 0 : (unsigned)std::min<int64_t>(MOST_GROUPS / 2, (grad.rows + zero_per - 1) / zero_per);
     ProfScope ps(ctx, ATOMO_K_EMBEDDING, stream);
     int at = 0;
