@@ -578,6 +578,14 @@ def _stream_of(ctx: Context, stream: Optional[torch.cuda.Stream]) -> int:
     return int(stream.cuda_stream)
 
 
+def _new(ctx: Context, shape, dtype: torch.dtype, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """A tensor for results of work on `stream`: the allocator gives out again what has been freed in that stream's order."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=ctx.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=ctx.device)
+
+
 def _on_device(ctx: Context, t: torch.Tensor, what: str, types) -> int:
     """Checks the type and the device of a tensor; returns its address."""
     if not isinstance(t, torch.Tensor) or t.dtype not in types:
@@ -636,7 +644,7 @@ def atomo_embedding(ctx: Context, table: torch.Tensor, tokens: torch.Tensor, sca
     Context.status() says so."""
     c_table, c_tokens = _pack_rows(ctx, table, "table"), _pack_tokens(ctx, tokens, padding)
     if out is None:
-        out = torch.empty(*tokens.shape, table.shape[1], dtype=table.dtype, device=table.device)
+        out = _new(ctx, (*tokens.shape, table.shape[1]), table.dtype, stream)
     c_out = _pack_rows(ctx, _as_rows(out, tokens, "out"), "out")
     _check(lib().atomo_embedding(ctx._h, c_table, c_tokens, scale, c_out, _stream_of(ctx, stream)), "atomo_embedding")
     return out
@@ -740,7 +748,7 @@ def atomo_adamw_grad_norm(ctx: Context, plan: AdamwPlan, grad_scale: float = 1.0
                           stream=None) -> torch.Tensor:
     """|grad_scale| times the Euclidean norm of all gradients of the plan, a float32 tensor [1] on the device."""
     if out is None:
-        out = torch.empty(1, dtype=torch.float32, device=ctx.device)
+        out = _new(ctx, (1,), torch.float32, stream)
     at = _flat(ctx, out, "out", _ONE_F32, 1)
     _check(lib().atomo_adamw_grad_norm(ctx._h, plan._h, grad_scale, at, _stream_of(ctx, stream)), "atomo_adamw_grad_norm")
     return out
@@ -774,7 +782,7 @@ def atomo_state8_unpack(ctx: Context, which: str, codes: torch.Tensor, scales: t
     codes_at, n = _flat(ctx, codes, "codes", u8), codes.numel()
     scales_at = _flat(ctx, scales, "scales", u8, -(-n // STATE8_BLOCK))
     if out is None:
-        out = torch.empty(n, dtype=torch.float32, device=codes.device)
+        out = _new(ctx, (n,), torch.float32, stream)
     out_at = _flat(ctx, out, "out", _TYPES, n)
     _check(lib().atomo_state8_unpack(ctx._h, ATOMO_STATE_M if which == "m" else ATOMO_STATE_V, codes_at, scales_at, n, _TYPES[out.dtype],
                                      out_at, _stream_of(ctx, stream)), "atomo_state8_unpack")

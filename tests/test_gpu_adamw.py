@@ -359,7 +359,7 @@ def test_on_another_stream_and_two_plans():
     side = torch.cuda.Stream()
     a, b = Model([70_001, 5], seed=1), Model([70_001, 5], seed=1)
     side.wait_stream(torch.cuda.current_stream())
-    norm = binding.atomo_adamw_grad_norm(ctx(), a.plan, out=torch.empty(1, device="cuda"), stream=side)
+    norm = binding.atomo_adamw_grad_norm(ctx(), a.plan, stream=side)
     binding.atomo_adamw_step(ctx(), a.plan, 1e-2, step=1, grad_norm=norm, max_norm=1.0, stream=side)
     side.synchronize()
     binding.atomo_adamw_step(ctx(), b.plan, 1e-2, step=1, grad_norm=binding.atomo_adamw_grad_norm(ctx(), b.plan), max_norm=1.0)
