@@ -75,9 +75,10 @@ def check_grad(tokens, dy, grad, scale=1.0, before=None, padding=-1):
         assert torch.equal(grad[~named], before[~named])
 
 
-# tokens, rows, columns: one of each, odd columns, single lanes, columns over a group of lanes, one row, many tokens
+# tokens, rows, columns: one of each, odd columns, single lanes, columns over a group of lanes, one row, many tokens; three digits to sort by; more
+# tokens than 64 parts of the sort take
 SIZES = [(1, 1, 1), (1, 50, 8), (7, 5, 3), (64, 33, 64), (65, 1000, 257), (300, 70, 511), (513, 129, 1030), (1000, 1, 40), (4097, 300, 72),
-         (16384, 5000, 33), (16385, 700, 16), (40_000, 200_003, 24), (100_001, 17, 130)]
+         (16384, 5000, 33), (16385, 700, 16), (40_000, 200_003, 24), (100_001, 17, 130), (9000, 600_001, 5), (1_100_001, 5000, 2)]
 
 
 @pytest.mark.parametrize("n, rows, cols", SIZES)
