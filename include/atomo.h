@@ -367,8 +367,8 @@ int atomo_embedding(atomo_ctx* ctx, const atomo_rows* table /*host*/, const atom
 /*
  * Its gradient: grad[r] = (accumulate ? grad[r] : 0) + scale * sum over the t with tokens[t] = r of dy[t], summed in
  * fp32 and rounded once to grad's type.  Without accumulate every row of grad is written, those that no token names as
- * zeros; with it such rows are not touched.  The order of the sum depends on the sizes and the tokens alone, so the same
- * call gives the same bits in every run.
+ * zeros; with it such rows are not touched.  The order of the sum depends on the sizes, types and tokens alone, so the
+ * same call gives the same bits in every run.
  *   dy : tokens->n rows (at least) of grad->cols columns.
  * Tokens outside of the table are left out, and reported as by atomo_embedding.
  */
@@ -422,8 +422,9 @@ typedef struct atomo_adamw_options {
 
 typedef struct atomo_adamw atomo_adamw;   /* opaque: the tensors of a model, described once on the device */
 
-/* Describes the tensors (HOST array of n, read during the call) on the context's device; waits for the device.  Memory that a step
- * writes may overlap nothing else in the plan: ATOMO_EINVAL, as for tensors of more than 6.8e10 elements together.  Contents stay the caller's: nothing of them is kept.
+/* Describes the tensors (HOST array of n, read during the call) on the context's device; waits for the device.  Memory that a
+ * step writes may overlap nothing else in the plan: ATOMO_EINVAL, as for more than 1.6e7 pieces of at most 2048 elements (3.4e10
+ * elements).  Contents stay the caller's: nothing of them is kept.
  * One plan must not be used from two streams at once.  Destroy it before its context, and after the graphs that hold its
  * calls. */
 int atomo_adamw_create(atomo_ctx* ctx, const atomo_adamw_tensor* tensors /*host*/, int n, atomo_adamw** out);
