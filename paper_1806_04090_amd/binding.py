@@ -690,8 +690,9 @@ def alloc_adamw_state(n: int, bits: int, device) -> AdamwState:
 
 
 class AdamwPlan:
-    """Parameters, gradients and states of a model, described once for all steps; the tensors stay the caller's and are kept
-    alive by the plan.  A tensor that is given other memory needs a new plan.
+    """Parameters, gradients and states of a model, described once for all steps.  The tensors stay the caller's.  The plan keeps
+    the memory alive that they had when it was made, and works on that: a tensor that is given other memory, or another tensor in
+    its place (in a list, or in an AdamwState), needs a new plan.  A graph that holds calls of a plan needs it as long as it is replayed.
 
     params: contiguous float32 tensors, or None for a plan of gradients alone (atomo_adamw_grad_norm); grads: float32, bfloat16 or
     float16 of the same sizes; copies: None, or for each tensor None or a bfloat16, float16 or float32 tensor that gets the rounded
@@ -709,24 +710,30 @@ class AdamwPlan:
         if (params is None) != (states is None):
             raise ValueError("parameters need states, and states parameters")
         f32, u8 = (torch.float32,), (torch.uint8,)
-        blob = []
+        blob, kept = [], []
+
+        def place(t, what, types, size=None):
+            at = _flat(ctx, t, what, types, size)
+            kept.append((t, t.detach()))         # (the memory itself as well: `t.data = other` takes it from t)
+            return at
+
         for j, g in enumerate(grads):
             size, at, copy_type = g.numel(), [0] * 6, ATOMO_F32
             if params is not None:
                 s = states[j]
-                at[0] = _flat(ctx, params[j], f"params[{j}]", f32, size)
+                at[0] = place(params[j], f"params[{j}]", f32, size)
                 if s.m_scale is None and s.v_scale is None:
-                    at[1], at[2] = (_flat(ctx, x, f"states[{j}]", f32, size) for x in (s.m, s.v))
+                    at[1], at[2] = (place(x, f"states[{j}]", f32, size) for x in (s.m, s.v))
                 else:
                     blocks = -(-size // STATE8_BLOCK)
-                    at[1:5] = [_flat(ctx, x, f"states[{j}]", u8, k) for x, k in
+                    at[1:5] = [place(x, f"states[{j}]", u8, k) for x, k in
                                ((s.m, size), (s.v, size), (s.m_scale, blocks), (s.v_scale, blocks))]
                 if copies[j] is not None:
-                    at[5] = _flat(ctx, copies[j], f"copies[{j}]", _TYPES, size)
+                    at[5] = place(copies[j], f"copies[{j}]", _TYPES, size)
                     copy_type = _TYPES[copies[j].dtype]
-            grad = _flat(ctx, g, f"grads[{j}]", _TYPES)
+            grad = place(g, f"grads[{j}]", _TYPES)
             blob.append(_PACK_ADAMW_TENSOR(size, at[0], grad, *at[1:], _TYPES[g.dtype], copy_type, mult[j], decay[j]))
-        self._tensors = (params, list(grads), states, copies)
+        self._tensors = kept
         _check(lib().atomo_adamw_create(ctx._h, b"".join(blob), n, C.byref(self._h)), "atomo_adamw_create")
 
     def close(self):

@@ -1,0 +1,107 @@
+"""CPU: what the binding's AdamwPlan keeps alive, with the library's calls replaced by ones that note their arguments."""
+import ctypes as C
+import gc
+import struct
+import weakref
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1806_04090_amd import binding
+
+
+class Library:
+    """Stands for the library: every call succeeds and is noted; contexts and plans are numbers."""
+
+    def __init__(self):
+        self.calls, self.handles = [], 0
+
+    def _create(self, name, args, out):
+        self.handles += 1
+        out._obj.value = self.handles
+        self.calls.append((name, *args, self.handles))
+        return 0
+
+    def atomo_create(self, out, device):
+        return self._create("create", (device,), out)
+
+    def atomo_adamw_create(self, ctx, blob, n, out):
+        return self._create("adamw_create", (ctx.value, blob, n), out)
+
+    def atomo_adamw_destroy(self, ctx, plan):
+        self.calls.append(("adamw_destroy", ctx.value, plan.value))
+        return 0
+
+    def atomo_destroy(self, ctx):
+        self.calls.append(("destroy", ctx.value))
+        return 0
+
+
+@pytest.fixture
+def library(monkeypatch):
+    library = Library()
+    monkeypatch.setattr(binding, "lib", lambda: library)
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    yield library
+    gc.collect()                                                 # (whatever is left ends while the library is still replaced)
+
+
+def context():
+    ctx = binding.Context(0)
+    ctx.index = -1                                               # what tensors in host memory give as their device
+    return ctx
+
+
+def eight_bit_model():
+    """Lists for a plan, and the arrays whose memory its tensors have."""
+    n = 300
+    arrays = [np.ones(n, np.float32), np.ones(n, np.float16), *(np.zeros(k, np.uint8) for k in (n, n, 3, 3)), np.ones(n, np.float32)]
+    p, g, m, v, m_scale, v_scale, copy = (torch.from_numpy(a) for a in arrays)
+    return ([p], [g], [binding.AdamwState(m, v, m_scale, v_scale)], [copy]), arrays
+
+
+def tensors_of(params, grads, states, copies):
+    s = states[0]
+    return [params[0], grads[0], s.m, s.v, s.m_scale, s.v_scale, copies[0]]
+
+
+def addresses(library):
+    """Those that the plan was made from: parameter, gradient, m, v, scales, copy."""
+    (blob,) = [call[2] for call in library.calls if call[0] == "adamw_create"]
+    return list(struct.unpack_from("7Q", blob, 8))
+
+
+def clear_lists(params, grads, states, copies):
+    for x in (params, grads, states, copies):
+        x.clear()
+
+
+def replace_in_lists(params, grads, states, copies):
+    params[0], grads[0], copies[0], states[0] = torch.ones(1), torch.ones(1), torch.ones(1), binding.alloc_adamw_state(1, 32, "cpu")
+
+
+def load_a_checkpoint(params, grads, states, copies):
+    for name in ("m", "v", "m_scale", "v_scale"):
+        setattr(states[0], name, getattr(states[0], name).clone())
+
+
+def give_other_memory(params, grads, states, copies):
+    for t in tensors_of(params, grads, states, copies):
+        t.data = torch.zeros_like(t)
+
+
+@pytest.mark.parametrize("change", [clear_lists, replace_in_lists, load_a_checkpoint, give_other_memory])
+def test_a_plan_keeps_the_memory_that_it_was_made_from(library, change):
+    ctx, (model, arrays) = context(), eight_bit_model()
+    at, memory = [a.ctypes.data for a in arrays], [weakref.ref(a) for a in arrays]
+    plan = binding.AdamwPlan(ctx, *model[:3], copies=model[3])
+    assert addresses(library) == at
+    del arrays
+    change(*model)
+    gc.collect()
+    assert all(a() is not None for a in memory)
+    plan.close()
+    del model
+    gc.collect()
+    assert all(a() is None for a in memory)                      # and no longer than it has to
