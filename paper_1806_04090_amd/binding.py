@@ -10,6 +10,7 @@ import ctypes as C
 import math
 import os
 import struct
+import weakref
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
 
@@ -315,17 +316,23 @@ def lq_capacity(n: int, q: float) -> int:
 # -------------------------------------------------------------------------------------- context
 
 class Context:
-    """Owns an atomo_ctx (device workspace, latched device flags) on one GPU."""
+    """Owns an atomo_ctx (device workspace, latched device flags) on one GPU.  Closing it closes its plans."""
 
     def __init__(self, device: int = 0):
+        self._h, self._plans = C.c_void_p(), {}                 # (of each plan: its handle, and the AdamwPlan if there still is one)
         if not torch.cuda.is_available():
             raise RuntimeError("libatomo needs a GPU: no HIP device is visible and there is no CPU fallback")
         self.device = torch.device("cuda", device)
         self.index = device
-        self._h = C.c_void_p()
         _check(lib().atomo_create(C.byref(self._h), device), "atomo_create")
 
     def close(self):
+        for handle, plan in list(self._plans.items()):
+            plan = plan()
+            if plan is not None:
+                plan.close()
+            else:                                # (one that has become garbage together with this context)
+                self._close_plan(handle)
         if self._h:
             lib().atomo_destroy(self._h)
             self._h = C.c_void_p()
@@ -335,6 +342,10 @@ class Context:
             self.close()
         except Exception:
             pass
+
+    def _close_plan(self, handle: int):
+        if self._plans.pop(handle, None) is not None:
+            lib().atomo_adamw_destroy(self._h, handle)
 
     def reserve(self, nbytes: int):
         _check(lib().atomo_reserve(self._h, nbytes), "atomo_reserve")
@@ -735,10 +746,11 @@ class AdamwPlan:
             blob.append(_PACK_ADAMW_TENSOR(size, at[0], grad, *at[1:], _TYPES[g.dtype], copy_type, mult[j], decay[j]))
         self._tensors = kept
         _check(lib().atomo_adamw_create(ctx._h, b"".join(blob), n, C.byref(self._h)), "atomo_adamw_create")
+        ctx._plans[self._h.value] = weakref.ref(self)
 
     def close(self):
-        if self._h and self._ctx._h:
-            lib().atomo_adamw_destroy(self._ctx._h, self._h)
+        if self._h:
+            self._ctx._close_plan(self._h.value)
         self._h, self._tensors = C.c_void_p(), None
 
     def __del__(self):

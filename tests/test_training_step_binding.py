@@ -27,10 +27,15 @@ class Library:
         return self._create("create", (device,), out)
 
     def atomo_adamw_create(self, ctx, blob, n, out):
+        if not ctx.value:
+            return binding.ATOMO_EINVAL
         return self._create("adamw_create", (ctx.value, blob, n), out)
 
+    def atomo_strerror(self, status):
+        return b"an error"
+
     def atomo_adamw_destroy(self, ctx, plan):
-        self.calls.append(("adamw_destroy", ctx.value, plan.value))
+        self.calls.append(("adamw_destroy", ctx.value, plan))
         return 0
 
     def atomo_destroy(self, ctx):
@@ -105,3 +110,51 @@ def test_a_plan_keeps_the_memory_that_it_was_made_from(library, change):
     del model
     gc.collect()
     assert all(a() is None for a in memory)                      # and no longer than it has to
+
+
+def names(library):
+    return [(call[0], *call[-1:]) for call in library.calls]
+
+
+def test_a_context_that_is_closed_closes_its_plans_first(library):
+    ctx, other = context(), context()                            # handles 1 and 2
+    (model, _), (second, _) = eight_bit_model(), eight_bit_model()
+    plan, gone, theirs = binding.AdamwPlan(ctx, *model[:3]), binding.AdamwPlan(ctx, None, second[1]), binding.AdamwPlan(other, None, model[1])
+    gone.close()
+    ctx.close()
+    assert names(library)[5:] == [("adamw_destroy", 4), ("adamw_destroy", 3), ("destroy", 1)]
+    plan.close()                                                 # nothing is left to do
+    ctx.close()
+    assert len(library.calls) == 8
+    with pytest.raises(binding.AtomoError):
+        binding.AdamwPlan(ctx, None, second[1])
+    theirs.close()
+    other.close()
+    assert names(library)[8:] == [("adamw_destroy", 5), ("destroy", 2)]
+
+
+def test_plans_and_contexts_that_nothing_holds_any_more(library):
+    ctx, (model, _) = context(), eight_bit_model()
+    plan = binding.AdamwPlan(ctx, *model[:3])
+    del ctx                                                      # the plan holds it
+    gc.collect()
+    assert len(library.calls) == 2
+    del plan
+    gc.collect()
+    assert names(library)[2:] == [("adamw_destroy", 2), ("destroy", 1)]
+
+
+def test_a_plan_and_its_context_in_one_piece_of_garbage(library):
+    class Trainer:
+        pass
+
+    for plan_first in (False, True):
+        t, (model, _), before = Trainer(), eight_bit_model(), len(library.calls)
+        t.me, t.ctx = t, context()
+        t.plan = binding.AdamwPlan(t.ctx, *model[:3])
+        if plan_first:
+            t.ctx.model = t
+        del t
+        gc.collect()
+        ctx, plan = library.calls[before][-1], library.calls[before + 1][-1]
+        assert names(library)[before + 2:] == [("adamw_destroy", plan), ("destroy", ctx)]
