@@ -383,7 +383,8 @@ int atomo_embedding_workspace_bytes(int64_t n_tokens, int64_t rows, int32_t cols
  *     g' = c g,  c = grad_scale * min(1, max_norm / *grad_norm)             (c = grad_scale without a norm to clip to)
  *     m = beta1 m + (1 - beta1) g'        v = beta2 v + (1 - beta2) g' g'
  *     param -= lr lr_mult / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps) + lr lr_mult weight_decay param
- * in fp32, every product and sum of m and v rounded by itself; and, if it has one, copy = param rounded to copy_type.
+ * in fp32 (eps rounded to it), every product and sum of m and v rounded by itself; and, if it has one, copy = param rounded to
+ * copy_type.  0 / 0, of an element without a gradient so far where eps is 0, counts as 0.
  * Where *grad_norm is not finite the step does nothing at all (the caller counts t on only where it was finite).
  *
  * States m and v are float32, or 8 bits per element with a scale for each block of 128 consecutive elements.  The scale

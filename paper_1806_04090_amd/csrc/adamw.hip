@@ -55,6 +55,7 @@ struct StepArgs {
     float b1, c1, b2, c2;              // beta and 1 - beta, rounded once each from double
     float eps, root;                   // root = 1 / sqrt(1 - beta2^t)
     float max_norm, grad_scale;
+    bool plain_eps;
 };
 
 __device__ double power(double x, long long t)
@@ -111,23 +112,33 @@ __device__ inline void average(const StepArgs& a, const Rates& r, float g, float
 // What `v` has to be for the instruction's square root, which takes numbers below the smallest normal one for zero.
 constexpr uint32_t SMALLEST_ROOT = 0x00800000u;
 
+// Whether denominators are numbers that the instruction's reciprocal takes and gives as they are, whatever v is: it takes those below the
+// smallest normal one for zero, and gives zero for what lies below it.  (The root with its factor is below 2^91.)
+inline bool plain_eps(float eps) { return eps >= 0x1p-126f && eps <= 0x1p125f; }
+
 // The parameters of N elements.  Root and reciprocal are those of the hardware, off by at most one unit in the last place each (the
-// update by 13 half units in all; the exact forms are some twenty instructions per element more).
+// update by 13 half units in all; the exact forms are some twenty instructions per element more), where v and eps are in their range.
 template <int N>
 __device__ inline void update(const StepArgs& a, const Rates& r, float (&p)[N], const float (&m)[N], const float (&v)[N])
 {
     uint32_t least = ~0u;                                        // of the v that are not zero, less one
 #pragma unroll
     for (int e = 0; e < N; ++e) least = min(least, __float_as_uint(v[e]) - 1);
-    const auto all = [&](auto root) {
+    const auto all = [&](auto quotient) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float step = r.rate * (m[e] * __builtin_amdgcn_rcpf(root(v[e]) * r.root + a.eps));
+            const float step = r.rate * quotient(m[e], v[e]);
             p[e] = p[e] - (step + r.decay * p[e]);
         }
     };
-    if (__any(least < SMALLEST_ROOT - 1)) all([](float x) { return sqrtf(x); });
-    else all([](float x) { return __builtin_amdgcn_sqrtf(x); });
+    if (!a.plain_eps || __any(least < SMALLEST_ROOT - 1)) {
+        all([&](float x, float y) {
+            const float d = sqrtf(y) * r.root + a.eps;
+            return x == 0.0f && d == 0.0f ? 0.0f : x / d;        // (an element that has had no gradient yet, with an eps of zero)
+        });
+    } else {
+        all([&](float x, float y) { return x * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(y) * r.root + a.eps); });
+    }
 }
 
 __device__ inline f32x4 load_any4(int type, const void* base, long long i)
@@ -680,6 +691,7 @@ int adamw_step(atomo_ctx* ctx, const atomo_adamw* plan, const atomo_adamw_option
     a.b2 = (float)o.beta2;
     a.c2 = (float)(1.0 - o.beta2);
     a.eps = (float)o.eps;
+    a.plain_eps = plain_eps(a.eps);
     a.max_norm = o.max_norm;
     a.grad_scale = o.grad_scale;
     ProfScope ps(ctx, ATOMO_K_ADAMW, stream);
