@@ -116,14 +116,13 @@ constexpr uint32_t SMALLEST_ROOT = 0x00800000u;
 // smallest normal one for zero, and gives zero for what lies below it.  (The root with its factor is below 2^91.)
 inline bool plain_eps(float eps) { return eps >= 0x1p-126f && eps <= 0x1p125f; }
 
-// The parameters of N elements.  Root and reciprocal are those of the hardware, off by at most one unit in the last place each (the
-// update by 13 half units in all; the exact forms are some twenty instructions per element more), where v and eps are in their range.
-template <int N>
+// The parameters of N elements.  Root and quotient are rounded once each.  FAST: where v and eps are in their range, root and reciprocal are
+// those of the hardware, off by at most one unit in the last place each, some twenty instructions per element less: the update is off by 13
+// half units in all instead of 12.  8-bit states take them (0.27 billion 0.72 ms, with the exact forms 0.84), whose codes are off
+// by far more; 32-bit states would gain 1.5 of 61.4 us where all lies in the last cache (ResNet-18, clipped) and nothing where it does not.
+template <bool FAST, int N>
 __device__ inline void update(const StepArgs& a, const Rates& r, float (&p)[N], const float (&m)[N], const float (&v)[N])
 {
-    uint32_t least = ~0u;                                        // of the v that are not zero, less one
-#pragma unroll
-    for (int e = 0; e < N; ++e) least = min(least, __float_as_uint(v[e]) - 1);
     const auto all = [&](auto quotient) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
@@ -131,14 +130,19 @@ __device__ inline void update(const StepArgs& a, const Rates& r, float (&p)[N], 
             p[e] = p[e] - (step + r.decay * p[e]);
         }
     };
-    if (!a.plain_eps || __any(least < SMALLEST_ROOT - 1)) {
-        all([&](float x, float y) {
-            const float d = sqrtf(y) * r.root + a.eps;
-            return x == 0.0f && d == 0.0f ? 0.0f : x / d;        // (an element that has had no gradient yet, with an eps of zero)
-        });
-    } else {
-        all([&](float x, float y) { return x * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(y) * r.root + a.eps); });
+    if constexpr (FAST) {
+        uint32_t least = ~0u;                                    // of the v that are not zero, less one
+#pragma unroll
+        for (int e = 0; e < N; ++e) least = min(least, __float_as_uint(v[e]) - 1);
+        if (a.plain_eps && !__any(least < SMALLEST_ROOT - 1)) {
+            all([&](float x, float y) { return x * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(y) * r.root + a.eps); });
+            return;
+        }
     }
+    all([&](float x, float y) {
+        const float d = sqrtf(y) * r.root + a.eps;
+        return x == 0.0f && d == 0.0f ? 0.0f : x / d;            // (an element that has had no gradient yet, with an eps of zero)
+    });
 }
 
 __device__ inline f32x4 load_any4(int type, const void* base, long long i)
@@ -186,7 +190,7 @@ __global__ __launch_bounds__(256) void adamw_states32(const Tensor* tensors, con
                 pe[e] = p4[e]; me[e] = m4[e]; ve[e] = v4[e];
                 average(a, r, g[e], me[e], ve[e]);
             }
-            update(a, r, pe, me, ve);
+            update<false>(a, r, pe, me, ve);
             const f32x4 new_p = {pe[0], pe[1], pe[2], pe[3]};
             store4<ATOMO_F32, true>(t.param, i, new_p);
             store4<ATOMO_F32, true>(m, i, f32x4{me[0], me[1], me[2], me[3]});
@@ -196,7 +200,7 @@ __global__ __launch_bounds__(256) void adamw_states32(const Tensor* tensors, con
             for (long long j = i; j < t.n; ++j) {
                 float pe[1] = {t.param[j]}, me[1] = {m[j]}, ve[1] = {v[j]};
                 average(a, r, load_any1(t.grad_type, t.grad, j), me[0], ve[0]);
-                update(a, r, pe, me, ve);
+                update<false>(a, r, pe, me, ve);
                 t.param[j] = pe[0];
                 m[j] = me[0];
                 v[j] = ve[0];
@@ -346,7 +350,7 @@ __global__ __launch_bounds__(256) void adamw_states8(const Tensor* tensors, cons
         sm = max(sm, __float_as_uint(m[e]) >> 23 & 0xff);
         sv = max(sv, __float_as_uint(v[e]) >> 23 & 0xff);
     }
-    update(a, r, p, m, v);
+    update<true>(a, r, p, m, v);
     const bool finite_all = !__any(sm == 0xff || sv == 0xff);
     if (!finite_all) {                                           // scales are those of the finite ones
         sm = sv = 0;

@@ -74,3 +74,19 @@ def test_a_denominator_of_eps_alone(bits, m, eps):
     want = -lr / (1 - B1) * B1 * m / eps32
     # b1 and its product, the quotient (its reciprocal off by 2 U, its product by U), the rate and its product: 7 U; the difference from zero is exact
     assert ((p.double() - want).abs() <= 7 * U * 1.01 * abs(want)).all()
+
+
+@pytest.mark.parametrize("eps", [0.0, 2.0 ** -20])
+def test_root_and_quotient_of_32_bit_states_are_rounded_once_each(eps):
+    # beta1 = 1/2, beta2 = 0, t = 1, lr = 1/2: m = (m + g) / 2, v = g^2, the rate is one and so is the factor of the root; from p = 0 the
+    # new p is the quotient itself, bit for bit the same as with numpy's float32
+    n = 100_003
+    g, m = normal(n, 5), normal(n, 6)
+    p, v = torch.zeros(n, device="cuda"), normal(n, 7).square()
+    plan = binding.AdamwPlan(ctx(), [p], [g], [binding.AdamwState(m, v)])
+    a, b = g.cpu().numpy(), m.cpu().numpy()
+    want_m, want_v = np.float32(0.5) * b + np.float32(0.5) * a, a * a
+    binding.atomo_adamw_step(ctx(), plan, 0.5, 0.5, 0.0, eps, step=1)
+    assert np.array_equal(m.cpu().numpy(), want_m) and np.array_equal(v.cpu().numpy(), want_v)
+    want = -(want_m / (np.sqrt(want_v) + np.float32(eps)))
+    assert want.dtype == np.float32 and np.array_equal(p.cpu().numpy(), want)
