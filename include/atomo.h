@@ -395,8 +395,14 @@ int atomo_embedding_workspace_bytes(int64_t n_tokens, int64_t rows, int32_t cols
  * thousandth, a code by an eighth): of an |x| that lies f steps of 2^-16 above a code, the next one is taken iff
  * r + f >= 2^16, r uniform in 0 .. 2^16 - 1.  A v that is not zero keeps a code that is not zero.  Infinite and NaN
  * values become NaN.  Element i of the tensor whose predecessors in the plan fill b blocks takes word i mod 4 of the Philox block with
- * counter (32 b + i div 4, t) and key seed: r is its low half for m, its high half for v.
+ * counter (32 b + i div 4, t) and key seed: r is its low half for m, its high half for v.  These are the words that an encoder
+ * draws for the coordinates of a message with the same seed and stream_id = t.  A coordinate that it keeps with probability p has
+ * a word below p 2^32, so that the r of its v would be below p 2^16, and its v rounded down but for a share of p: the expectation holds only
+ * if the seed is none of those of the messages that the gradients come from (whose stream ids may equal t).  Where a program has one seed for all,
+ * this one is ATOMO_ADAMW_SEED ^ that seed.
  */
+#define ATOMO_ADAMW_SEED 0x6164616d775f6d76ull
+
 typedef struct atomo_adamw_tensor {
     int64_t n;                       /* elements, 0 < n < 2^40                                        */
     float* param;                    /* [n]; NULL (in every tensor of a plan): atomo_adamw_grad_norm only */
@@ -418,7 +424,7 @@ typedef struct atomo_adamw_options {
     const float* grad_norm;          /* device [1], optional: see above                               */
     float max_norm;                  /* > 0: clip to it (needs grad_norm); 0: do not clip             */
     float grad_scale;                /* finite                                                        */
-    uint64_t seed;                   /* of the rounding of 8-bit states                               */
+    uint64_t seed;                   /* of the rounding of 8-bit states: not one of an encoder's      */
 } atomo_adamw_options;
 
 typedef struct atomo_adamw atomo_adamw;   /* opaque: the tensors of a model, described once on the device */

@@ -26,6 +26,7 @@ ATOMO_KIND_SVD, ATOMO_KIND_ENTRYWISE, ATOMO_KIND_LQ = 0, 1, 2
 ATOMO_F32, ATOMO_BF16, ATOMO_F16 = 0, 1, 2
 ATOMO_STATE_M, ATOMO_STATE_V = 0, 1
 STATE8_BLOCK = 128           # elements of an 8-bit state that share a scale
+ATOMO_ADAMW_SEED = 0x6164616d775f6d76    # with a program's seed, by exclusive or: a seed of the rounding apart from those of its messages
 
 
 class AtomoError(RuntimeError):
@@ -774,14 +775,15 @@ def atomo_adamw_grad_norm(ctx: Context, plan: AdamwPlan, grad_scale: float = 1.0
 
 
 def atomo_adamw_step(ctx: Context, plan: AdamwPlan, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, *, step,
-                     grad_scale: float = 1.0, grad_norm: Optional[torch.Tensor] = None, max_norm: float = 0.0, seed: int = 0,
+                     grad_scale: float = 1.0, grad_norm: Optional[torch.Tensor] = None, max_norm: float = 0.0, seed: int = ATOMO_ADAMW_SEED,
                      stream=None) -> None:
     """One AdamW step of all tensors of the plan, in place (atomo.h has the formulas).
 
     step: t = 1, 2, ..., a number or an int64 tensor [1] on the device; lr: a number or a float32 tensor [1] on the
     device (a captured step reads such tensors at every replay).  grad_norm: what atomo_adamw_grad_norm gave for the
     same grad_scale; the step does nothing where it is not finite, and clips to max_norm if that is above 0.  seed: of the rounding
-    of 8-bit states."""
+    of 8-bit states; not one that messages are encoded with (with the same seed, a coordinate that a message kept would have its v rounded down):
+    ATOMO_ADAMW_SEED ^ the program's own, for instance."""
     step_at = lr_at = 0
     if isinstance(step, torch.Tensor):
         step, step_at = 0, _flat(ctx, step, "step", _ONE_I64, 1)

@@ -1,6 +1,9 @@
 """CPU: what the binding's AdamwPlan keeps alive, with the library's calls replaced by ones that note their arguments."""
 import ctypes as C
 import gc
+import inspect
+import os
+import re
 import struct
 import weakref
 
@@ -158,3 +161,9 @@ def test_a_plan_and_its_context_in_one_piece_of_garbage(library):
         gc.collect()
         ctx, plan = library.calls[before][-1], library.calls[before + 1][-1]
         assert names(library)[before + 2:] == [("adamw_destroy", plan), ("destroy", ctx)]
+
+
+def test_the_seed_of_the_rounding_is_the_same_in_the_header_and_no_small_number(library):
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "atomo.h")).read()
+    assert int(re.search(r"#define ATOMO_ADAMW_SEED (0x[0-9a-f]+)ull", text)[1], 16) == binding.ATOMO_ADAMW_SEED >= 2 ** 62
+    assert inspect.signature(binding.atomo_adamw_step).parameters["seed"].default == binding.ATOMO_ADAMW_SEED
