@@ -443,8 +443,8 @@ int atomo_adamw_grad_norm(atomo_ctx* ctx, const atomo_adamw* plan, float grad_sc
 
 int atomo_adamw_step(atomo_ctx* ctx, const atomo_adamw* plan, const atomo_adamw_options* opt /*host*/, void* stream);
 
-/* What 8-bit states stand for: out[i] = code times scale, rounded to `type` (exact in ATOMO_F32, and in ATOMO_BF16 down to
- * its smallest normal number).  n elements from the start of a block, 0 < n < 2^34. */
+/* What 8-bit states stand for: out[i] = code times scale, formed in fp32 and rounded to `type` (what a step has
+ * written is exact in ATOMO_F32, and in ATOMO_BF16 down to its smallest normal number).  n elements from the start of a block, 0 < n < 2^34. */
 enum { ATOMO_STATE_M = 0, ATOMO_STATE_V = 1 };
 int atomo_state8_unpack(atomo_ctx* ctx, int which, const uint8_t* codes, const uint8_t* scales, int64_t n, int type,
                         void* out, void* stream);
