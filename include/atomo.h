@@ -330,7 +330,7 @@ int atomo_apply_svd_batch(atomo_ctx* ctx, const atomo_svd_msg* msgs, const int32
  * The paper's own step is plain SGD (atomo_apply_svd_batch).
  *
  * Buffers that a call writes may not overlap others of that call.  Pointers need the alignment of their element type
- * only.  All calls below may be captured into a graph, atomo_adamw_create apart.  Those that need the context's
+ * only.  All calls below may be captured into a graph, atomo_adamw_create and atomo_adamw_destroy apart.  Those that need the context's
  * workspace (atomo_embedding_grad) do not grow it then: reserve it before (ATOMO_ENOMEM otherwise).  A block of
  * workspace that a captured call uses stays allocated until atomo_destroy, also when a later call makes the context
  * take a larger one; graphs of one context share it and must not run at the same time.  A captured call holds the
