@@ -5,8 +5,8 @@
 // The tensors of a plan are described once on the device; a step is one launch over chunks of CHUNK elements of all of
 // them (two, if both kinds of states occur).
 // Parameters, gradients and states go past the caches, both ways (0.27 billion parameters with bf16 gradients and copies, 28 bytes each:
-// 1.42 ms, 5.3 TB/s, through them; 1.28 ms, 5.9 TB/s, so; loads alone or stores alone gain nothing).  That takes whole cache lines
-// per row of lanes: with eight neighbouring elements per lane and half a line per store, 8-bit states went from 0.85 ms to 1.2.
+// 1.31 ms, 5.7 TB/s; through the caches 1.39; with 8-bit states 0.73 and 0.79).  That takes whole cache lines per row of lanes: with eight
+// neighbouring elements per lane and half a line per store, 8-bit states were slower by two fifths past the caches than through them.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -118,7 +118,7 @@ inline bool plain_eps(float eps) { return eps >= 0x1p-126f && eps <= 0x1p125f; }
 
 // The parameters of N elements.  Root and quotient are rounded once each.  FAST: where v and eps are in their range, root and reciprocal are
 // those of the hardware, off by at most one unit in the last place each, some twenty instructions per element less: the update is off by 13
-// half units in all instead of 12.  8-bit states take them (0.27 billion 0.72 ms, with the exact forms 0.84), whose codes are off
+// half units in all instead of 12.  8-bit states take them (0.27 billion 0.73 ms, with the exact forms 0.79), whose codes are off
 // by far more; 32-bit states would gain 1.5 of 61.4 us where all lies in the last cache (ResNet-18, clipped) and nothing where it does not.
 template <bool FAST, int N>
 __device__ inline void update(const StepArgs& a, const Rates& r, float (&p)[N], const float (&m)[N], const float (&v)[N])

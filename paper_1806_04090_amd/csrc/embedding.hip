@@ -109,8 +109,9 @@ __device__ inline void add(Cols<VEC>& a, const Cols<VEC>& b)
 // Lookup: lanes_x threads side by side on a row, ROWS rows of theirs on their way together
 // ---------------------------------------------------------------------------------------------
 
-// Sixteen bytes of the output per lane and store, whole lines per wave, which the caches need not keep: 65,536 rows of 2048 from bf16 to
-// bf16 86 -> 60 us, from fp32 97 -> 90.  (Eight columns per lane to fp32, two stores of half a line each: 156 -> 193.)
+// Sixteen bytes of the output per lane and store, whole lines per wave, which the caches need not keep (with eight columns per lane, fp32
+// takes two stores of half a line each, and was slower past the caches than through them by a quarter).  Two rows of a thread on their way: 65,536
+// rows of 2048 from bf16 to bf16 68 us, one row 100, four 66; to fp32 97, 163 and 106; from fp32 to bf16 89, 101 and 95.
 constexpr int TWO_ROWS = 2, MANY_GROUPS = 4096;
 
 template <int IN, int OUT, int ROWS>
@@ -160,7 +161,7 @@ __device__ inline uint32_t key_of(const Tokens& t, long long token, int rows, in
 
 // Up to RANKED tokens: the place of each is the number of those in front of it, by comparison with all.  One launch; n^2 comparisons.
 // A workgroup has 32 tokens, one per lane of each half of its sixteen waves, and the halves share out the keys to compare with.
-// (8192 tokens of 512 columns: 38 us for all of the gradient, 47 with the sort by digits; 12,288: 53, 49.)
+// (8192 tokens of 512 columns into 32,768 rows: 37 us for all of the gradient, 47 with the sort by digits; 12,288: 52, 49.)
 constexpr int RANKED = 8192, RANK_TOKENS = 32;
 
 template <int SOURCE>
@@ -505,8 +506,7 @@ __device__ void zero_rows(const uint32_t* keys, int n, uint32_t first, int per, 
 }
 
 // Waves of the first workgroups take a piece and a tile of columns each; the workgroups behind them write the zeros.  (On a stream of their
-// own beside the sort, with a byte per row for what the tokens name, the zeros slowed the sort's loads by more than they gained: 170 us
-// for 32,768 tokens into 65,536 x 2048, 174 so.)
+// own beside the sort, with a byte per row for what the tokens name, they made no difference beyond 3 %, and needed a second stream.)
 template <int IN, int OUT, int VEC, bool ACC>
 __global__ __launch_bounds__(256) void sum_pieces(Pieces s, const void* dy, long long ld_dy, Grad g, int pieces, int tiles, unsigned groups, int zero_per)
 {
