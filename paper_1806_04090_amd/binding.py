@@ -726,7 +726,7 @@ class AdamwPlan:
 
         def place(t, what, types, size=None):
             at = _flat(ctx, t, what, types, size)
-            kept.append((t, t.detach()))         # (the memory itself as well: `t.data = other` takes it from t)
+            kept.append((t, t.untyped_storage()))   # (the memory itself as well: `t.data = other` takes it from t)
             return at
 
         for j, g in enumerate(grads):
